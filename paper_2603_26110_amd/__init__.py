@@ -461,3 +461,6 @@ def calibrate_rotation(x: torch.Tensor):
     sg = torch.empty((nh, 64), dtype=torch.float32, device=x.device)
     _check(L.tq_calibrate_rotation(_ptr(x), nh, ncal, _ptr(pi), _ptr(sg), _stream(x.device)))
     return pi, sg
+
+
+from . import paged  # noqa: E402  (it takes this module's errors and flags)

@@ -1,4 +1,4 @@
-"""Build libturboesm.so (HIP, gfx950) in the package directory.
+"""Build libturboesm.so and libturboesm_paged.so (HIP, gfx950) in the package directory.
 
     python -m paper_2603_26110_amd.build
 
@@ -18,8 +18,11 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libturboesm.so")
+LIB_PAGED = os.path.join(PKG, "libturboesm_paged.so")
 SOURCES = ["tq_api.hip", "tq_quantize.hip", "tq_decode.hip", "tq_dequant.hip", "tq_calibrate.hip",
            "tq_probe.hip"]
+# The paged 8-bit cache is a library of its own, with a header of its own.
+SOURCES_PAGED = ["paged_api.hip", "paged_pages.hip", "paged_append.hip", "paged_attend.hip"]
 ARCH = os.environ.get("TQ_OFFLOAD_ARCH", "gfx950")
 
 CFLAGS = [
@@ -49,16 +52,21 @@ def _compile(src: str) -> str:
     return obj
 
 
-def build() -> str:
-    os.makedirs(OBJ_DIR, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=min(4, len(SOURCES))) as ex:
-        objs = list(ex.map(_compile, SOURCES))
-    tmp = LIB + ".tmp"
+def _link(objs: list[str], lib: str) -> None:
+    tmp = lib + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}{r.stderr}")
-    os.replace(tmp, LIB)
+    os.replace(tmp, lib)
+
+
+def build() -> str:
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    with ThreadPoolExecutor(max_workers=4) as ex:
+        objs = list(ex.map(_compile, SOURCES + SOURCES_PAGED))
+    _link(objs[:len(SOURCES)], LIB)
+    _link(objs[len(SOURCES):], LIB_PAGED)
     return LIB
 
 

@@ -1,0 +1,640 @@
+// Attention over the paged 8-bit cache (tqp_attend).
+//
+// One pass over a sequence's pages with the running maximum and sum of a
+// softmax, on the matrix cores with fp16 operands (every e4m3 value is an fp16
+// value) and binary32 sums. Both products are formed transposed:
+//   S^T = K Q^T   (A: keys, a token per row; B: queries, a row per column)
+//   O^T = V^T P^T (A: values, a dimension per row; B: weights)
+// A lane of the result of the first holds scores of one query row (its column)
+// for tokens 4 g + r of every group of 16 or 8, and the second product takes
+// its B operand from the same lane as long as the tokens are counted in that
+// order. The value plane is laid out in that order, so weights go from one
+// product to the next in registers, a row's maximum and sum need one or two
+// lane swaps, and rescaling is a multiplication by a value of the lane's own.
+//
+// Two kernels. For few rows a unit (one query token per sequence and its
+// group of heads) the cache is read once and bounds the time: tiles of 16 rows
+// (v_mfma_f32_16x16x32_f16), a page per wave, the waves of a block and, where
+// there are few units, several blocks share a sequence. For many rows the
+// arithmetic bounds it: 32 rows per wave (v_mfma_f32_32x32x16_f16).
+//
+// Rounding: q' and the weights round to fp16 (2^-11). That is 8 times finer
+// than a bf16 output; for an fp16 output q' is taken in two parts (the error
+// of a score grows with the score), for an fp32 output the weights too.
+#include <algorithm>
+
+#include "paged_device.hpp"
+
+namespace tqp {
+namespace {
+
+constexpr int kRowsFew = 16, kRowsMany = 32;
+constexpr int kMaxSplit = 64;
+constexpr int kPartRow = kDim + 2;                    // m, l, o[64] of a row
+constexpr int kPart = kRowsFew * kPartRow;            // floats of a block's partial
+// The largest weight is kept between 2^7 and 2^15: the reference of the exponents
+// is 7 below the running maximum and moves when a score is 15 above it. So
+// rescaling is rare, and the steps that fp16 has at its lower end, 2^-24, are
+// 2^-31 of the largest weight.
+constexpr float kTop = 7.0f, kRaise = 15.0f;
+
+__device__ __forceinline__ float lowest() { return -3.40282347e38f; }
+
+// Eight codes as fp16.
+__device__ __forceinline__ f16x8 halves8(uint32_t lo, uint32_t hi) {
+  const u32x4 w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true))};
+  return __builtin_bit_cast(f16x8, w);
+}
+
+__device__ __forceinline__ float max_across32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
+  return fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
+}
+__device__ __forceinline__ float max_across16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(x), __float_as_int(x), false, false);
+  return fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
+}
+
+template <int IO>
+__device__ __forceinline__ void store_one(const AttendArgs& a, int64_t at, float x) {
+  if (IO == kF32 || a.out_f32) reinterpret_cast<float*>(a.out)[at] = x;
+  else if (IO == kF16) reinterpret_cast<_Float16*>(a.out)[at] = (_Float16)x;
+  else reinterpret_cast<__bf16*>(a.out)[at] = (__bf16)x;
+}
+
+template <int IO>
+__device__ __forceinline__ void store_four(const AttendArgs& a, int64_t at, float x0, float x1, float x2, float x3) {
+  if (IO == kF32 || a.out_f32) {
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = make_float4(x0, x1, x2, x3);
+  } else if (IO == kF16) {
+    typedef _Float16 T __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<T*>(reinterpret_cast<_Float16*>(a.out) + at) = T{(_Float16)x0, (_Float16)x1, (_Float16)x2, (_Float16)x3};
+  } else {
+    typedef __bf16 T __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<T*>(reinterpret_cast<__bf16*>(a.out) + at) = T{(__bf16)x0, (__bf16)x1, (__bf16)x2, (__bf16)x3};
+  }
+}
+
+// One sequence's rows and length as a block finds them.
+struct Sequence {
+  int row0, n, len;
+  bool there, fine;
+};
+
+__device__ __forceinline__ Sequence sequence_of(const AttendArgs& a, int b) {
+  Sequence s;
+  s.row0 = a.row0[b];
+  const int end = a.row0[b + 1];
+  s.len = a.seq_len[b];
+  s.there = s.row0 >= 0 && end > s.row0 && end <= a.rows;
+  s.n = end - s.row0;
+  s.fine = s.len >= 0 && s.len <= a.max_len && s.len <= (int64_t)a.width * kPage && s.n <= a.max_new;
+  return s;
+}
+
+// NaN in all rows of a sequence, for the heads that share one key/value head.
+template <int IO>
+__device__ void refuse(const AttendArgs& a, const Sequence& s, int l, int h) {
+  const int width = a.group * kDim;
+  for (int64_t i = threadIdx.x; i < (int64_t)s.n * width; i += blockDim.x)
+    store_one<IO>(a, (((int64_t)l * a.rows + s.row0 + i / width) * a.heads + (int64_t)h * a.group) * kDim + i % width,
+                  __builtin_nanf(""));
+}
+
+// A query row: its place and how many tokens it sees.
+struct Row {
+  int row, head, pos, sees;
+  bool there, fine;
+};
+
+__device__ __forceinline__ Row row_of(const AttendArgs& a, const Sequence& s, int h, int f) {
+  Row r;
+  r.there = f < s.n * a.group;
+  const int tok = r.there ? f / a.group : 0;
+  r.row = s.row0 + tok;
+  r.head = h * a.group + (r.there ? f - tok * a.group : 0);
+  r.pos = a.pos[r.row];
+  r.fine = r.there && r.pos >= 0 && (!a.cs || r.pos < a.rope_positions);
+  r.sees = !r.fine ? 0 : a.causal ? min(s.len, r.pos + 1) : s.len;
+  return r;
+}
+
+// Dimensions d0 .. d0+N-1 of a row, rotated (their partners are among them, or
+// 32 away in the half pairing).
+template <int IO, int N>
+__device__ __forceinline__ void load_query(const AttendArgs& a, const Row& r, int l, int d0, float (&x)[N]) {
+  const int64_t at = l * a.q.layer + r.row * a.q.row + r.head * a.q.head;
+  load_elements<IO>(a.q.data, at + d0, x);
+  if (!a.cs || !r.fine) return;
+  const float2* cs = reinterpret_cast<const float2*>(a.cs) + (int64_t)r.pos * (kDim / 2);
+  if (a.rope_half) {
+    float o[N];
+    load_elements<IO>(a.q.data, at + (d0 ^ 32), o);
+    const bool second = (d0 & 32) != 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float2 c = cs[(d0 & 31) + i];
+      x[i] = second ? o[i] * c.y + x[i] * c.x : x[i] * c.x - o[i] * c.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 c = cs[(d0 + i) >> 1];
+      const float p = x[i] * c.x - x[i + 1] * c.y, q = x[i] * c.y + x[i + 1] * c.x;
+      x[i] = p;
+      x[i + 1] = q;
+    }
+  }
+}
+
+// The exponent of a row's largest entry (from its bits): a row over 2^e has
+// entries up to 2 in fp16, whatever the type's range. Rows of zeros, and what
+// is no number, stay as they are.
+__device__ __forceinline__ int row_exponent(uint32_t amax) {
+  return amax < 0x00800000u || amax >= kInfBits ? 0 : (int)(amax >> 23) - 127;
+}
+
+// x 2^-e in two steps (e may be -126 .. 127).
+__device__ __forceinline__ float over_pow2(float x, int e) {
+  return x * pow2(-(e >> 1)) * pow2(-(e - (e >> 1)));
+}
+
+template <int PREC>
+__device__ __forceinline__ void split8(const float* x, int e, f16x8& hi, f16x8& lo) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = over_pow2(x[i], e);
+    hi[i] = (_Float16)v;
+    if (PREC > 0) lo[i] = (_Float16)(v - (float)hi[i]);
+  }
+}
+
+// What a sum of products is multiplied by: positive and finite, so that masked
+// scores stay -infinity and zeros stay zero.
+__device__ __forceinline__ float score_scale(float row, float page) {
+  return __builtin_amdgcn_fmed3f(row * page, 1e-37f, 3e38f);
+}
+
+// Bytes of the tokens first .. first+3 that are below len.
+__device__ __forceinline__ uint32_t below(int first, int len) {
+  const int n = len - first;
+  return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+}
+
+// ------------------------------------------------------------- few rows
+template <int IO, int PREC, int W>
+__global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, int per_xcd, int tiles) {
+  constexpr int kStride = kDim + 4;
+  __shared__ float s_m[W][kRowsFew], s_l[W][kRowsFew];
+  __shared__ __align__(16) float s_o[W * kRowsFew * kStride];
+  __shared__ int s_last;
+  // Blocks go to the XCDs in turn; a unit's blocks are neighbours on one.
+  const int work = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
+  if (work >= total) return;
+  const int unit = work / a.nsplit, split = work - unit * a.nsplit;
+  const int tile = unit % tiles, rest = unit / tiles;
+  const int h = rest % a.kv_heads, b = (rest / a.kv_heads) % a.B, l = rest / a.kv_heads / a.B;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, g = lane >> 4, c16 = lane & 15;
+  const Sequence s = sequence_of(a, b);
+  if (!s.there) return;
+  if (!s.fine) {
+    if (tile == 0 && split == 0) refuse<IO>(a, s, l, h);
+    return;
+  }
+  const int f0 = tile * kRowsFew, rows = min(s.n * a.group - f0, kRowsFew);
+  if (rows <= 0) return;
+  const Row r = row_of(a, s, h, f0 + c16);
+  int most = r.sees, least = r.fine ? r.sees : INT_MAX;
+#pragma unroll
+  for (int o = 8; o >= 1; o >>= 1) {
+    most = max(most, __shfl_xor(most, o, 64));
+    least = min(least, __shfl_xor(least, o, 64));
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
+  const int ntiles = (most + kPage - 1) / kPage;
+  const int st = max((ntiles + a.nsplit - 1) / a.nsplit, W);
+  const int parts = max((ntiles + st - 1) / st, 1);
+  if (split >= parts) return;
+  const int begin = split * st + wave, end = min(ntiles, (split + 1) * st);
+
+  // q': lane (g, column) has dimensions 16 g .. 16 g + 15 of its row
+  f16x8 qh[2], ql[2];
+  float rowscale;
+  {
+    float x[16];
+    load_query<IO>(a, r, l, 16 * g, x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, abs_bits(x[i]));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+    const int e = row_exponent(m);
+    split8<PREC>(x, e, qh[0], ql[0]);
+    split8<PREC>(x + 8, e, qh[1], ql[1]);
+    rowscale = a.scale2 * pow2(max(e, -126));
+  }
+
+  const int64_t region = ((int64_t)(a.layer0 + l) * a.kv_heads + h) * a.cache.pages;
+  const uint8_t* kplane = a.cache.k + region * kPageBytes + lane * 16;
+  const uint8_t* vplane = a.cache.v + region * kPageBytes + lane * 16;
+  const float2* scales = reinterpret_cast<const float2*>(a.cache.scales) + region;
+  const int32_t* table = a.table + (int64_t)b * a.width;
+
+  float m = lowest(), lsum = 0.0f, vscale = 1.0f;
+  f32x4 O[4] = {};
+
+  struct Raw {
+    u32x4 k[4], v[4];
+    float2 sc;
+  };
+  int entries = 0;               // lane i: the table's entry of the wave's i-th page of 64
+  auto load = [&](Raw& w, int i) {
+    int page = __builtin_amdgcn_readlane(entries, i);
+    const bool bad = page < 0 || page >= a.cache.pages;
+    page = bad ? 0 : page;
+    const int64_t at = (int64_t)page * kPageBytes;
+    // keys: row c16 of the 16 tokens of part i, its bytes 16 g .. 16 g + 15
+    const uint8_t* kp = kplane - lane * 16 + at + c16 * kDim + g * 16;
+    // values: dimension 16 i + c16, the sixteen tokens of group g
+    const uint8_t* vp = vplane - lane * 16 + at + g * 1024 + c16 * 16;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w.k[j] = *reinterpret_cast<const u32x4*>(kp + j * 1024);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w.v[j] = *reinterpret_cast<const u32x4*>(vp + j * 256);
+    w.sc = scales[page];
+    if (bad) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w.k[j] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+    }
+  };
+  auto attend = [&](Raw& w, int tl) {
+    f32x4 S[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f16x8 k0 = halves8(w.k[i][0], w.k[i][1]), k1 = halves8(w.k[i][2], w.k[i][3]);
+      f32x4 z = {};
+      if (PREC > 0) {
+        z = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, ql[0], z, 0, 0, 0);
+        z = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, ql[1], z, 0, 0, 0);
+      }
+      z = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qh[0], z, 0, 0, 0);
+      S[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qh[1], z, 0, 0, 0);
+    }
+    const float c = score_scale(rowscale, w.sc.x);
+    const int tok0 = tl * kPage + 4 * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) S[i] *= c;
+    if ((tl + 1) * kPage > least) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (tok0 + 16 * i + j >= r.sees) S[i][j] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t keep = below(tok0 + 16 * i, s.len);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w.v[j][i] &= keep;
+      }
+    }
+    float top = S[0][0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top = fmaxf(top, S[i][j]);
+    top = max_across16(max_across32(top));
+    if (__any(top > m + kRaise)) {
+      const float next = top > m + kRaise ? top - kTop : m;
+      const float f = __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      lsum *= f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) O[i] *= f;
+    }
+    if (w.sc.y != vscale) {      // (uniform: O is in units of the page's value scale)
+      const float f = vscale / w.sc.y;
+      vscale = w.sc.y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) O[i] *= f;
+    }
+    f16x8 ph[2], pl[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = __builtin_amdgcn_exp2f(S[i][j] - m);
+        lsum += p;
+        ph[i >> 1][4 * (i & 1) + j] = (_Float16)p;
+        if (PREC > 1) pl[i >> 1][4 * (i & 1) + j] = (_Float16)(p - (float)(_Float16)p);
+      }
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const f16x8 v0 = halves8(w.v[d][0], w.v[d][1]), v1 = halves8(w.v[d][2], w.v[d][3]);
+      if (PREC > 1) {
+        O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pl[0], O[d], 0, 0, 0);
+        O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pl[1], O[d], 0, 0, 0);
+      }
+      O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, ph[0], O[d], 0, 0, 0);
+      O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, ph[1], O[d], 0, 0, 0);
+    }
+  };
+  for (int first = begin; first < end; first += 64 * W) {
+    const int n = min(64, (end - first + W - 1) / W);
+    entries = lane < n ? table[first + lane * W] : 0;
+    Raw cur, next;
+    load(cur, 0);
+    for (int i = 0; i < n; ++i) {
+      if (i + 1 < n) load(next, i + 1);
+      attend(cur, first + i * W);
+      cur = next;
+    }
+  }
+  lsum += __shfl_xor(lsum, 16, 64);
+  lsum += __shfl_xor(lsum, 32, 64);
+  if (g == 0) {
+    s_m[wave][c16] = m;
+    s_l[wave][c16] = lsum;
+  }
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+    *reinterpret_cast<f32x4*>(s_o + (wave * kRowsFew + c16) * kStride + 16 * d + 4 * g) = O[d] * vscale;
+  __syncthreads();
+
+  float* part = a.partials + ((int64_t)unit * a.nsplit + split) * kPart;
+  for (int e = t; e < rows * kDim; e += W * 64) {
+    const int q = e / kDim, d = e % kDim;
+    float M = lowest(), L = 0.0f, o = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[w][q]);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][q] - M);
+      L += s_l[w][q] * f;
+      o += s_o[(w * kRowsFew + q) * kStride + d] * f;
+    }
+    if (parts > 1) {
+      __hip_atomic_store(part + q * kPartRow + 2 + d, o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (d == 0) {
+        __hip_atomic_store(part + q * kPartRow, M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(part + q * kPartRow + 1, L, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    } else {
+      const Row x = row_of(a, s, h, f0 + q);
+      store_one<IO>(a, (((int64_t)l * a.rows + x.row) * a.heads + x.head) * kDim + d,
+                    !x.fine ? __builtin_nanf("") : L == 0.0f ? 0.0f : o / L);
+    }
+  }
+  if (parts == 1) return;
+
+  // The partials are stored past the caches of the XCDs; once they are there
+  // this block counts itself in, and the last one to do so joins them all.
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (t == 0)
+    s_last = __hip_atomic_fetch_add(a.counters + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)parts - 1;
+  __syncthreads();
+  if (!s_last) return;
+  const float* base = a.partials + (int64_t)unit * a.nsplit * kPart;
+  float* s_f = s_o;              // [row][part] weights (16 x 64 at most)
+  float* s_lp = s_o + kRowsFew * kMaxSplit;
+  static_assert(W * kRowsFew * kStride >= 2 * kRowsFew * kMaxSplit, "room for the weights");
+  for (int e = t; e < rows * parts; e += W * 64) {
+    const int q = e / parts, p = e - q * parts;
+    s_f[q * kMaxSplit + p] = __hip_atomic_load(base + (int64_t)p * kPart + q * kPartRow, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_lp[q * kMaxSplit + p] = __hip_atomic_load(base + (int64_t)p * kPart + q * kPartRow + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  for (int e = t; e < rows * kDim; e += W * 64) {
+    const int q = e / kDim, d = e % kDim;
+    float M = lowest(), L = 0.0f, o = 0.0f;
+    for (int p = 0; p < parts; ++p) M = fmaxf(M, s_f[q * kMaxSplit + p]);
+    const float* src = base + q * kPartRow + 2 + d;
+    for (int p0 = 0; p0 < parts; p0 += 8) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[j] = __hip_atomic_load(src + (int64_t)min(p0 + j, parts - 1) * kPart, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (p0 + j >= parts) break;
+        const float f = __builtin_amdgcn_exp2f(s_f[q * kMaxSplit + p0 + j] - M);
+        L += s_lp[q * kMaxSplit + p0 + j] * f;
+        o += v[j] * f;
+      }
+    }
+    const Row x = row_of(a, s, h, f0 + q);
+    store_one<IO>(a, (((int64_t)l * a.rows + x.row) * a.heads + x.head) * kDim + d,
+                  !x.fine ? __builtin_nanf("") : L == 0.0f ? 0.0f : o / L);
+  }
+  if (t == 0) __hip_atomic_store(a.counters + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// ------------------------------------------------------------ many rows
+template <int IO, int PREC>
+__global__ __launch_bounds__(256) void attend_many(AttendArgs a, int total, int per_xcd, int tiles) {
+  const int work = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
+  if (work >= total) return;
+  // (the last rows first: under a causal mask they see the most)
+  const int tile = tiles - 1 - work % tiles, rest = work / tiles;
+  const int h = rest % a.kv_heads, b = (rest / a.kv_heads) % a.B, l = rest / a.kv_heads / a.B;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, c32 = lane & 31;
+  const Sequence s = sequence_of(a, b);
+  if (!s.there) return;
+  if (!s.fine) {
+    if (tile == 0) refuse<IO>(a, s, l, h);
+    return;
+  }
+  const int f0 = (tile * 4 + wave) * kRowsMany;
+  if (f0 >= s.n * a.group) return;
+  const Row r = row_of(a, s, h, f0 + c32);
+  int most = r.sees, least = r.fine ? r.sees : INT_MAX;
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) {
+    most = max(most, __shfl_xor(most, o, 64));
+    least = min(least, __shfl_xor(least, o, 64));
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
+  const int ntiles = (most + kPage - 1) / kPage;
+
+  // q': lane (half, column) has dimensions 32 half .. +31 of its row
+  f16x8 qh[4], ql[4];
+  float rowscale;
+  {
+    float x[32];
+    load_query<IO>(a, r, l, 32 * half, x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = max(m, abs_bits(x[i]));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+    const int e = row_exponent(m);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split8<PREC>(x + 8 * i, e, qh[i], ql[i]);
+    rowscale = a.scale2 * pow2(max(e, -126));
+  }
+  const int64_t region = ((int64_t)(a.layer0 + l) * a.kv_heads + h) * a.cache.pages;
+  const uint8_t* kplane = a.cache.k + region * kPageBytes + c32 * kDim + half * 32;
+  const uint8_t* vplane = a.cache.v + region * kPageBytes + half * 1024 + c32 * 16;
+  const float2* scales = reinterpret_cast<const float2*>(a.cache.scales) + region;
+  const int32_t* table = a.table + (int64_t)b * a.width;
+
+  float m = lowest(), lsum = 0.0f, vscale = 1.0f;
+  f32x16 O[2] = {};
+  struct Raw {
+    u32x4 k[2][2], v[2][2];      // [tokens 32 T ..][half of the row's part]; [dimensions 32 t ..][groups half, half + 2]
+    float2 sc;
+  };
+  auto load = [&](Raw& w, int tl) {
+    int page = table[tl];
+    const bool bad = page < 0 || page >= a.cache.pages;
+    page = bad ? 0 : page;
+    const uint8_t* kp = kplane + (int64_t)page * kPageBytes;
+    const uint8_t* vp = vplane + (int64_t)page * kPageBytes;
+#pragma unroll
+    for (int T = 0; T < 2; ++T)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        w.k[T][j] = *reinterpret_cast<const u32x4*>(kp + T * 2048 + j * 16);
+        w.v[T][j] = *reinterpret_cast<const u32x4*>(vp + T * 512 + j * 2048);
+      }
+    w.sc = scales[page];
+    if (bad) {
+#pragma unroll
+      for (int T = 0; T < 2; ++T)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) w.k[T][j] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+    }
+  };
+  auto attend = [&](Raw& w, int tl) {
+    f32x16 S[2];
+#pragma unroll
+    for (int T = 0; T < 2; ++T) {
+      f32x16 z = {};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f16x8 kf = halves8(w.k[T][i >> 1][2 * (i & 1)], w.k[T][i >> 1][2 * (i & 1) + 1]);
+        if (PREC > 0) z = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[i], z, 0, 0, 0);
+        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[i], z, 0, 0, 0);
+      }
+      S[T] = z;
+    }
+    const float c = score_scale(rowscale, w.sc.x);
+    const bool edge = (tl + 1) * kPage > least;
+    if (edge) {
+#pragma unroll
+      for (int T = 0; T < 2; ++T)
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (tl * kPage + 32 * T + 8 * (j >> 2) + 4 * half + (j & 3) >= r.sees) S[T][j] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t keep = below(tl * kPage + 16 * i + 4 * (half + 2 * j), s.len);
+          w.v[0][j][i] &= keep;
+          w.v[1][j][i] &= keep;
+        }
+    }
+    float top = S[0][0];
+#pragma unroll
+    for (int T = 0; T < 2; ++T)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) top = fmaxf(top, S[T][j]);
+    top = max_across32(top) * c;
+    if (__any(top > m + kRaise)) {
+      const float next = top > m + kRaise ? top - kTop : m;
+      const float f = __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      lsum *= f;
+      O[0] *= f;
+      O[1] *= f;
+    }
+    if (w.sc.y != vscale) {
+      const float f = vscale / w.sc.y;
+      vscale = w.sc.y;
+      O[0] *= f;
+      O[1] *= f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      f16x8 ph, pl;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(S[u >> 1][8 * (u & 1) + j], c, -m));
+        lsum += p;
+        ph[j] = (_Float16)p;
+        if (PREC > 1) pl[j] = (_Float16)(p - (float)ph[j]);
+      }
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const f16x8 vf = halves8(w.v[d][0][u], w.v[d][1][u]);
+        if (PREC > 1) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl, O[d], 0, 0, 0);
+        O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph, O[d], 0, 0, 0);
+      }
+    }
+  };
+  if (ntiles > 0) {
+    Raw cur, next;
+    load(cur, 0);
+    for (int tl = 0; tl < ntiles; ++tl) {
+      if (tl + 1 < ntiles) load(next, tl + 1);
+      attend(cur, tl);
+      cur = next;
+    }
+  }
+  lsum += __shfl_xor(lsum, 32, 64);
+  if (!r.there) return;
+  const float f = !r.fine ? __builtin_nanf("") : lsum == 0.0f ? 0.0f : vscale / lsum;
+  const int64_t at = (((int64_t)l * a.rows + r.row) * a.heads + r.head) * kDim + 4 * half;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      store_four<IO>(a, at + 32 * d + 8 * i, O[d][4 * i] * f, O[d][4 * i + 1] * f, O[d][4 * i + 2] * f, O[d][4 * i + 3] * f);
+}
+
+}  // namespace
+
+AttendPlan plan_attend(int64_t units0, int64_t rows, int max_len) {
+  AttendPlan p{};
+  p.few = rows <= 64;
+  const int per = p.few ? kRowsFew : 4 * kRowsMany;
+  p.tiles = (int)((rows + per - 1) / per);
+  p.units = units0 * p.tiles;
+  p.nsplit = 1;
+  p.waves = 4;
+  if (!p.few) return p;
+  const int64_t pages = std::max<int64_t>((max_len + (int64_t)kPage - 1) / kPage, 1);
+  // Blocks of four waves, about four per compute unit, every wave with a page.
+  const int64_t want = std::max<int64_t>(1024 / std::max<int64_t>(p.units, 1), 1);
+  p.nsplit = (int)std::min<int64_t>(std::min<int64_t>(want, (pages + p.waves - 1) / p.waves), kMaxSplit);
+  if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * kPart * sizeof(float);
+  return p;
+}
+
+namespace {
+
+template <int IO, int PREC>
+hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  const int64_t total = p.units * p.nsplit, per_xcd = (total + kXcds - 1) / kXcds;
+  const dim3 grid((unsigned)(per_xcd * kXcds));
+  if (p.few)
+    hipLaunchKernelGGL((attend_few<IO, PREC, 4>), grid, dim3(256), 0, st, a, (int)total, (int)per_xcd, p.tiles);
+  else
+    hipLaunchKernelGGL((attend_many<IO, PREC>), grid, dim3(256), 0, st, a, (int)total, (int)per_xcd, p.tiles);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  if (a.io == kF32) return launch<kF32, 2>(a, p, st);
+  if (a.io == kF16) return a.out_f32 ? launch<kF16, 2>(a, p, st) : launch<kF16, 1>(a, p, st);
+  return a.out_f32 ? launch<kBF16, 2>(a, p, st) : launch<kBF16, 0>(a, p, st);
+}
+
+}  // namespace tqp

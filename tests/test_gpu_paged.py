@@ -1,0 +1,606 @@
+"""The paged 8-bit cache on the GPU against plain 64-bit implementations (tests/paged_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as ref
+import paper_2603_26110_amd as tq
+from paper_2603_26110_amd import paged
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+# ------------------------------------------------------------------ pages
+def pool_of(state, total):
+    pool = paged.PagePool(total)
+    n = len(state.stack)
+    pool.stack[:n] = i32(state.stack) if n else pool.stack[:0]
+    pool.state[0] = n
+    return pool
+
+
+def check_pool(pool, state, table, seq_len):
+    n = int(pool.state[0])
+    assert pool.state.tolist() == [len(state.stack), 0, 0, 0]
+    assert pool.stack[:n].tolist() == state.stack
+    assert table.tolist() == state.table and seq_len.tolist() == state.len
+
+
+@pytest.mark.parametrize("B,longest,most,width,spare", [
+    (1, 0, 1, 1, 5), (1, 63, 1, 1, 0), (1, 64, 1, 2, 1), (1, 64, 1, 1, 1), (3, 500, 700, 20, 100),
+    (64, 1000, 1, 17, 64), (64, 1000, 1, 17, 7), (257, 130, 300, 7, 400), (1000, 0, 90, 2, 1500), (1000, 3, 40, 2, 300),
+    (4096, 70, 3, 2, 200), (5, 0, 5000, 80, 400)])
+def test_assign_and_release(B, longest, most, width, spare):
+    g = np.random.default_rng(B * 1000 + most)
+    lens = np.minimum(g.integers(0, longest + 1, B), width * 64)
+    new = g.integers(0, most + 1, B)
+    held = [ref.pages_of(int(n)) for n in lens]
+    total = sum(held) + spare
+    ids = g.permutation(total).tolist()
+    table, at = [], 0
+    for h in held:
+        table.append(ids[at:at + h] + [-1] * (width - h))
+        at += h
+    state = ref.Pool(ids[at:], table, lens.tolist())
+    pool, t, n = pool_of(state, total), i32(table).reshape(B, width), i32(lens.tolist())
+    if spare == 0:
+        state.stack = []
+        pool.state[0] = 0
+    rows = int(new.sum()) + int(g.integers(0, 5))
+    for step in range(3):
+        got = paged.assign(pool, t, n, i32(new.tolist()), rows)
+        want = state.assign(new.tolist(), rows, total)
+        for name, a, b in zip(("slots", "pos", "row0", "granted"), got, want):
+            assert a.tolist() == b, (step, name)
+        check_pool(pool, state, t, n)
+        keep = [int(x) for x in g.integers(-1, np.maximum(np.array(state.len), 1) + 2)]
+        if step == 1:
+            keep = [0 if i % 2 else x for i, x in enumerate(keep)]
+        paged.release(pool, t, n, i32(keep))
+        state.release(keep)
+        check_pool(pool, state, t, n)
+        new = np.minimum(g.integers(0, most + 1, B), np.maximum(rows // B, 1))
+
+
+def test_assign_refuses_what_is_not_valid():
+    # negative lengths and counts, a length past the table, rows that do not fit; the others go on
+    total, width = 40, 3
+    lens = [10, -1, 0, 190, 64 * 3 + 1, 5, 20]
+    new = [60, 3, -4, 3, 1, 64, 7]
+    table = [[39, -1, -1], [-1] * 3, [-1] * 3, [36, 35, 34], [0, 1, 2], [33, -1, -1], [32, -1, -1]]
+    state = ref.Pool(list(range(3, 30)), table, lens)
+    pool, t, n = pool_of(state, total), i32(table), i32(lens)
+    rows = 60 + 3 + 3 + 1 + 64 + 6
+    got = paged.assign(pool, t, n, i32(new), rows)
+    want = state.assign(new, rows, total)
+    assert want[3] == [1, 0, 0, 0, 0, 1, 0] and want[2][-1] == rows
+    for a, b in zip(got, want):
+        assert a.tolist() == b
+    check_pool(pool, state, t, n)
+    paged.release(pool, t, n, i32([0] * 7))
+    state.release([0] * 7)
+    check_pool(pool, state, t, n)
+
+
+def test_assign_with_a_bad_page_and_no_rows():
+    pool, t, n = paged.PagePool(8), i32([[99, -1], [-5, -1]]), i32([3, 64])
+    slots, pos, row0, granted = paged.assign(pool, t, n, i32([4, 2]), 6)
+    assert slots.tolist() == [-1] * 4 + [0, 1] and pos.tolist() == [3, 4, 5, 6, 64, 65] and granted.tolist() == [1, 1]
+    slots, pos, row0, granted = paged.assign(pool, t, n, i32([0, 0]), 0)
+    assert slots.numel() == 0 and row0.tolist() == [0, 0, 0] and granted.tolist() == [1, 1]
+    empty = torch.empty((0, 2), dtype=torch.int32, device=DEV)
+    slots, pos, row0, granted = paged.assign(pool, empty, empty[:, 0].contiguous(), empty[:, 0].contiguous(), 3)
+    assert slots.tolist() == [-1] * 3 and row0.tolist() == [0] and granted.numel() == 0
+    paged.release(pool, empty, empty[:, 0].contiguous(), empty[:, 0].contiguous())
+    assert pool.state.tolist() == [7, 0, 0, 0]
+
+
+# ----------------------------------------------------------------- append
+def random_cache(L, H, pages, seed):
+    """A cache whose pages hold codes of all sizes and assorted scales."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    c = paged.Cache(L, H, pages)
+    for t in (c.k_codes, c.v_codes):
+        t.copy_(torch.randint(0, 127, t.shape, generator=g, device=DEV) + 128 * torch.randint(0, 2, t.shape, generator=g, device=DEV))
+    c.scales.copy_(2.0 ** torch.randint(-12, 3, c.scales.shape, generator=g, device=DEV).float())
+    return c
+
+
+def same_cache(cache, want):
+    k, v, s = cache.values()
+    assert np.array_equal(np.round(np.log2(s.double().cpu().numpy())).astype(int), want.e)
+    assert np.array_equal(2.0 ** want.e.astype(np.float32), s.cpu().numpy())
+    for name, a, b in (("k", k, want.k), ("v", v.reshape(k.shape), want.v)):
+        a = a.double().cpu().numpy()
+        wrong = ~((a == b) | (np.isnan(a) & np.isnan(b)))
+        assert not wrong.any(), (name, int(wrong.sum()), np.argwhere(wrong)[:5], a[wrong][:5], b[wrong][:5])
+
+
+def rope_of(kind, positions=700):
+    return None if kind == "none" else tq.rope_table(positions)
+
+
+def rows_tensor(x, dtype, fused):
+    """x [nl][rows][H][64] of the type; fused: as a slice of a wider tensor."""
+    x = x.to(dtype)
+    if not fused:
+        return x.contiguous()
+    nl, rows, H = x.shape[:3]
+    wide = torch.full((nl, rows + 3, H + 5, 64), float("nan"), dtype=dtype, device=DEV)
+    wide[:, 1:rows + 1, 2:H + 2] = x
+    return wide[:, 1:rows + 1, 2:H + 2]
+
+
+def slots_of(runs, pages, seed):
+    """Slots of runs (first slot within a page, tokens), each run over pages of its own; and positions."""
+    ids = np.random.default_rng(seed).permutation(pages).tolist()
+    slots, pos = [], []
+    for at, n in runs:
+        page = ids.pop()
+        for j in range(n):
+            if j and (at + j) % 64 == 0:
+                page = ids.pop()
+            slots.append(page * 64 + (at + j) % 64)
+            pos.append(at + j)
+    return slots, pos
+
+
+RUNS = {
+    "one": [(0, 1)], "one_later": [(17, 1)], "few": [(5, 4), (62, 5), (0, 3), (63, 1), (60, 4)],
+    "page": [(0, 64)], "pages": [(0, 200)], "later": [(37, 150)], "short_of_a_page": [(1, 63)],
+    "decode": [(i % 64, 1) for i in range(130)],
+    "ragged": [(0, 7), (63, 66), (30, 1), (0, 129), (12, 30), (3, 5), (0, 64), (40, 24)],
+}
+
+
+@pytest.mark.parametrize("dtype,rope,fused", [(F16, "pairs", False), (F16, "half", True), (BF16, "pairs", True),
+                                              (BF16, "none", False), (F32, "half", False), (F32, "pairs", True)])
+@pytest.mark.parametrize("runs", list(RUNS))
+def test_append(runs, dtype, rope, fused):
+    L, H, nl, layer0 = 3, 3, 2, 1
+    seed = len(runs) * 7 + len(RUNS[runs])
+    pages = sum(ref.pages_of(a + n) for a, n in RUNS[runs]) + 3
+    slots, pos = slots_of(RUNS[runs], pages, seed)
+    cache = random_cache(L, H, pages, seed)
+    want = ref.CacheRef(cache)
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    N = len(slots)
+    # (sizes over many powers of two, so that some pages' scales grow and others do not)
+    size = 2.0 ** torch.randint(-9, 6, (nl, N, H, 1), generator=g, device=DEV).float()
+    k = rows_tensor(torch.randn((nl, N, H, 64), generator=g, device=DEV) * size, dtype, fused)
+    v = rows_tensor(torch.randn((nl, N, H, 64), generator=g, device=DEV) * size.flip(1), dtype, fused)
+    cs = rope_of(rope)
+    params = paged.Params(L, 2 * H, H, cs, dtype, flags=paged.ROPE_HALF if rope == "half" else 0)
+    paged.append(params, cache, k, v, torch.tensor(slots, device=DEV), i32(pos), layer0=layer0)
+    want.append(k.float().cpu().numpy(), v.float().cpu().numpy(), slots, pos, None if cs is None else cs.cpu().numpy(),
+                rope == "half", layer0)
+    same_cache(cache, want)
+
+
+@pytest.mark.parametrize("count", [1, 3, 40, 64])
+def test_append_of_what_is_no_number(count):
+    for which in range(4):
+        cache = random_cache(1, 2, 6, 50 + which)
+        want = ref.CacheRef(cache)
+        g = torch.Generator(device=DEV).manual_seed(count)
+        k, v = torch.randn((2, 1, count, 2, 64), generator=g, device=DEV).unbind(0)
+        at = 64 - count if which % 2 else 0
+        slots = [3 * 64 + at + j for j in range(count)]
+        bad = [float("nan"), float("inf"), float("-inf"), 3e38][which]
+        k[0, count // 2, 0, 5] = bad                       # (3e38 stays finite unless RoPE overflows it)
+        k[0, count // 2, 0, 4] = bad if which == 3 else 1.0
+        v[0, count - 1, 1, 63] = float("inf")
+        cs = tq.rope_table(64)
+        params = paged.Params(1, 2, 2, cs, F32)
+        pos = [at + j for j in range(count)]
+        paged.append(params, cache, k, v, torch.tensor(slots, device=DEV), i32(pos))
+        want.append(k.cpu().numpy(), v.cpu().numpy(), slots, pos, cs.cpu().numpy(), False)
+        same_cache(cache, want)
+
+
+@pytest.mark.parametrize("size", [0.0, 1e-45, 1e-20, 2.0 ** -48 * 448, 448.0, 448.0001, 464.0, 65504.0, 1e15, 1e30])
+@pytest.mark.parametrize("count", [2, 33])
+def test_append_over_the_range(size, count):
+    cache = paged.Cache(1, 1, 2)
+    want = ref.CacheRef(cache)
+    x = torch.linspace(-1, 1, count * 64, device=DEV).view(1, count, 1, 64) * size
+    slots = list(range(64, 64 + count))
+    params = paged.Params(1, 1, 1, None, F32)
+    paged.append(params, cache, x, -x, torch.tensor(slots, device=DEV), i32(slots))
+    want.append(x.cpu().numpy(), -x.cpu().numpy(), slots, slots, None, False)
+    same_cache(cache, want)
+
+
+def test_append_skips_rows_that_are_not_there():
+    pages = 8
+    cache = random_cache(1, 2, pages, 9)
+    want = ref.CacheRef(cache)
+    slots = [-1, 64, 65, -7, 66, pages * 64, 2 ** 40, 130, 131, 200, 201, 202]
+    pos = [0, 1, 2, 3, 4, 5, 6, -1, 9, 99, 100, 3]       # (a table of 100 positions: -1 and 100 are out of it)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    k, v = torch.randn((2, 1, len(slots), 2, 64), generator=g, device=DEV).half().unbind(0)
+    cs = tq.rope_table(100)
+    params = paged.Params(1, 2, 2, cs, F16)
+    paged.append(params, cache, k, v, torch.tensor(slots, device=DEV), i32(pos))
+    want.append(k.float().cpu().numpy(), v.float().cpu().numpy(), slots, pos, cs.cpu().numpy(), False)
+    same_cache(cache, want)
+    before = [t.clone() for t in (cache.k_codes, cache.v_codes, cache.scales)]
+    paged.append(params, cache, k, v, torch.full((len(slots),), -1, dtype=torch.int64, device=DEV), i32(pos))
+    paged.append(params, cache, k[:, :0], v[:, :0], torch.empty(0, dtype=torch.int64, device=DEV), i32([]))
+    assert all(torch.equal(a, b) for a, b in zip(before, (cache.k_codes, cache.v_codes, cache.scales)))
+
+
+def test_append_token_by_token_and_at_once():
+    # the same page either way, but for codes that were rounded once more when the scale grew
+    g = torch.Generator(device=DEV).manual_seed(4)
+    k, v = torch.randn((2, 1, 150, 2, 64), generator=g, device=DEV).unbind(0)
+    params = paged.Params(1, 2, 2, None, F32)
+    slots = torch.arange(150, device=DEV)
+    whole, steps = paged.Cache(1, 2, 3), paged.Cache(1, 2, 3)
+    want = ref.CacheRef(steps)
+    paged.append(params, whole, k, v, slots, slots.int())
+    for t in range(150):
+        one = slice(t, t + 1)
+        paged.append(params, steps, k[:, one], v[:, one], slots[one], slots[one].int())
+        want.append(k[:, one].cpu().numpy(), v[:, one].cpu().numpy(), [t], [t], None, False)
+    same_cache(steps, want)
+    assert torch.equal(whole.scales, steps.scales)
+
+
+# ----------------------------------------------------------------- attend
+class World:
+    """Sequences with pages in random order, a cache of random codes, query rows."""
+
+    def __init__(self, lens, new, heads, kv_heads, dtype=F16, rope="pairs", layers=1, seed=0, out_f32=False,
+                 fused=False, spare=3, positions=None, scale=0.125):
+        self.lens, self.new, self.dtype, self.rope, self.scale = lens, new, dtype, rope, scale
+        B = len(lens)
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        held = [ref.pages_of(n) for n in lens]
+        self.pages = sum(held) + spare
+        ids = torch.randperm(self.pages, generator=torch.Generator().manual_seed(seed)).tolist()
+        self.width = max(held + [1])
+        self.table = []
+        for h in held:
+            self.table.append(ids[:h] + [-1] * (self.width - h))
+            ids = ids[h:]
+        self.rows = sum(new)
+        self.row0 = np.concatenate([[0], np.cumsum(new)]).tolist()
+        self.pos = [n - m + j for n, m in zip(lens, new) for j in range(m)]
+        self.cache = paged.Cache(layers, kv_heads, self.pages)
+        c = self.cache
+        shape = (layers, kv_heads, self.pages, 64, 64)
+        for t, gain in ((c.k_codes, 1.0), (c.v_codes, 1.0)):
+            x = torch.randn(shape, generator=g, device=DEV) * 60
+            t.copy_(x.to(torch.float8_e4m3fn).view(torch.uint8).view(t.shape))
+        e = torch.randint(-8, -5, c.scales.shape, generator=g, device=DEV)
+        c.scales.copy_(2.0 ** e.float())
+        self.q = rows_tensor(torch.randn((layers, self.rows, heads, 64), generator=g, device=DEV), dtype, fused)
+        self.cs = rope_of(rope, positions or max(lens + [1]) + 64)
+        flags = (paged.ROPE_HALF if rope == "half" else 0) | (paged.OUT_FP32 if out_f32 else 0)
+        self.params = paged.Params(layers, heads, kv_heads, self.cs, dtype, flags, softmax_scale=scale)
+        self.out_dtype = F32 if out_f32 else dtype
+        self.prec = 2 if self.out_dtype is F32 else 1 if dtype is F16 else 0
+
+    def call(self, causal=True, **kw):
+        args = dict(q=self.q, pos=i32(self.pos), row0=i32(self.row0), table=i32(self.table), seq_len=i32(self.lens),
+                    max_new=max(self.new + [1]), max_len=max(self.lens), causal=causal)
+        args.update(kw)
+        return paged.attend(self.params, self.cache, **args)
+
+    def want(self, causal=True):
+        k, v, s = self.cache.values()
+        k = k.double() * s[..., 0].double()[..., None, None]
+        v = v.reshape(k.shape).double() * s[..., 1].double()[..., None, None]
+        cs = None
+        if self.cs is not None:
+            ang = torch.arange(self.cs.shape[0], dtype=torch.float64)[:, None] * 10000.0 ** (
+                -torch.arange(32, dtype=torch.float64) / 32)
+            cs = torch.polar(torch.ones_like(ang), ang).to(DEV)
+        return ref.attend(k, v, self.q.double(), self.pos, self.row0, self.table, self.lens, causal, self.scale, cs,
+                          self.rope == "half")
+
+    def check(self, got, causal=True):
+        assert got.dtype is self.out_dtype and got.shape == self.q.shape
+        want, spread, size = self.want(causal)
+        # the table of cos and sin is in fp32: one more rounding of each, which the bound on a score has room for
+        tol = ref.bound(want, spread, size, max(self.lens), self.prec, self.out_dtype)
+        far = (got.double() - want).abs() / tol
+        number = torch.isfinite(want)
+        assert torch.equal(got.isnan(), ~number) and float(far[number].max()) <= 1.0, float(far[number].max())
+
+
+SHAPES = [   # lens, new, heads, kv_heads
+    ([1], [1], 1, 1), ([64], [1], 2, 1), ([65], [1], 3, 3), ([63, 1, 128], [1, 1, 1], 8, 2),
+    ([1025], [1], 4, 4), ([4000], [1], 5, 1), ([700, 0, 3, 64], [1, 1, 1, 1], 20, 20), ([300, 5], [1, 1], 16, 1),
+    ([900], [1], 48, 2), ([100, 200, 65], [3, 0, 5], 6, 2), ([200], [16], 4, 1), ([333, 77], [9, 33], 7, 7),
+    ([64], [64], 2, 2), ([65, 40], [65, 40], 4, 1), ([500], [129], 3, 1), ([130, 9000], [130, 70], 2, 1),
+    ([257, 64, 1, 600], [200, 64, 1, 300], 10, 2), ([2000], [31], 33, 3),
+]
+
+
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+@pytest.mark.parametrize("dtype,rope,out_f32,fused", [(F16, "pairs", False, False), (BF16, "half", False, True),
+                                                      (F32, "none", False, True), (BF16, "pairs", True, False),
+                                                      (F16, "none", True, True)])
+def test_attend(shape, dtype, rope, out_f32, fused):
+    w = World(*SHAPES[shape], dtype=dtype, rope=rope, out_f32=out_f32, fused=fused, layers=1 + shape % 2, seed=shape)
+    for causal in (True, False):
+        w.check(w.call(causal), causal)
+
+
+@pytest.mark.parametrize("new", [1, 80])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_that_see_nothing(new, causal):
+    w = World([0, 70, 0], [new, new, new], 4, 2, seed=1)
+    w.pos = [0] * new + [69] * new + list(range(new))       # queries of an empty cache, at positions of their own
+    got = w.call(causal)
+    w.check(got, causal)
+    assert bool((got[:, :new] == 0).all()) and bool((got[:, 2 * new:] == 0).all()) and bool(got[:, new:2 * new].any())
+
+
+def test_attend_layers_and_long_sequences():
+    w = World([8192, 5000], [1, 1], 8, 4, layers=3, seed=5)
+    got = w.call()
+    w.check(got)
+    # a call of one layer, and another of the same workspace, give the same
+    ws = torch.zeros(paged.workspace_bytes(w.params, 3, 2, 1, 8192), dtype=torch.uint8, device=DEV)
+    assert ws.numel() > 0
+    for _ in range(3):
+        for l in range(3):
+            one = w.call(q=w.q[l:l + 1], layer0=l, workspace=torch.zeros(1 << 22, dtype=torch.uint8, device=DEV))
+            assert (one.float() - got[l:l + 1].float()).abs().max() <= 2.0 ** -9 * got.float().abs().max()
+        assert torch.equal(w.call(workspace=ws), got)
+    assert int(ws[:16384].sum()) == 0
+
+
+@pytest.mark.parametrize("new", [1, 40, 200])
+def test_rows_and_sequences_that_are_refused(new):
+    lens, news = [400, 300, 200, 250, 220], [new, min(new, 300), min(new, 200), min(new, 3), min(new, 220)]
+    w = World(lens, news, 4, 2, seed=new)
+    fine = w.call()
+    w.check(fine)
+    out = torch.full((1, w.rows + 4, 4, 64), 7.0, dtype=F16, device=DEV)
+    q = torch.cat([w.q[:, :1], w.q, w.q[:, :3]], 1)
+    pos, row0 = [0] + w.pos + [0] * 3, [r + 1 for r in w.row0]
+    table = [list(r) for r in w.table]
+    table[2][1] = w.pages                        # the second page of sequence 2
+    lens = list(w.lens)
+    lens[1] = 10 ** 6
+    last = row0[4] - 1
+    pos[last] = -1                               # the last row of sequence 3
+    w.call(q=q, pos=i32(pos), row0=i32(row0), table=i32(table), seq_len=i32(lens), out=out)
+    assert bool((out[:, :1] == 7).all()) and bool((out[:, row0[-1]:] == 7).all())
+    same = lambda a, b: torch.equal(out[:, a:b], fine[:, a - 1:b - 1])
+    assert same(row0[0], row0[1]) and same(row0[3], last) and same(row0[4], row0[5])
+    assert bool(out[:, row0[1]:row0[2]].isnan().all()) and bool(out[:, last:last + 1].isnan().all())
+    sees = torch.tensor([p >= 64 for p in pos[row0[2]:row0[3]]])
+    part = out[:, row0[2]:row0[3]]
+    assert bool(part[:, sees].isnan().all()) and torch.equal(part[:, ~sees], fine[:, row0[2] - 1:row0[3] - 1][:, ~sees])
+    # a negative length, a length past the table, more rows than max_new, a position past the RoPE table
+    for bad in (-1, w.width * 64 + 1):
+        lens = list(w.lens)
+        lens[0] = bad
+        got = w.call(seq_len=i32(lens), max_len=10 ** 6)
+        assert bool(got[:, :w.row0[1]].isnan().all()) and bool(torch.isfinite(got[:, w.row0[1]:]).all())
+    if new > 3:
+        got = w.call(max_new=3)
+        assert bool(got[:, :w.row0[3]].isnan().all()) and bool(torch.isfinite(got[:, w.row0[3]:w.row0[4]]).all())
+    got = w.call(pos=i32([w.cs.shape[0]] + w.pos[1:]))
+    assert bool(got[:, :1].isnan().all()) and torch.equal(got[:, 1:], fine[:, 1:])
+    # rows of a sequence that row0 puts outside: skipped
+    out.fill_(7.0)
+    w.call(row0=i32([-1] + w.row0[1:5] + [w.rows + 1]), out=out[:, :w.rows].contiguous())
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_what_is_masked_may_hold_anything(new):
+    w = World([130, 190], [new, new], 4, 2, seed=8, dtype=BF16)
+    k, v, s = w.cache.values()
+    fine = w.call()
+    w.check(fine)
+    for b in range(2):                            # codes past the sequence's end
+        page, at = w.table[b][-1], w.lens[b] % 64
+        k[:, :, page, at:] = torch.full_like(k[:, :, page, at:], float("nan"))
+        for t in range(at, 64):
+            v[:, :, page, t // 16, t // 4 % 4, t % 4] = torch.full((1, 2, 64), float("nan"), device=DEV).to(v.dtype)
+    assert torch.equal(w.call(), fine)
+    # a key that is no number (as append writes it): the rows before its token do not see it
+    if new > 1:
+        t = w.lens[0] - 50
+        k[:, :, w.table[0][t // 64], t % 64] = torch.full((1, 2, 64), float("nan"), device=DEV).to(k.dtype)
+        got = w.call()
+        first = w.row0[0] + t - (w.lens[0] - new)
+        assert torch.equal(got[:, :first], fine[:, :first]) and torch.equal(got[:, w.row0[1]:], fine[:, w.row0[1]:])
+        assert bool(got[:, first:w.row0[1]].isnan().all())
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_scores_and_scales_of_all_sizes(new):
+    # large scores (one weight takes all), tiny ones, and pages whose scales are far apart
+    for gain, dtype in ((1e4, F16), (1e-6, F32), (1e30, BF16)):
+        w = World([200], [new], 2, 1, dtype=dtype, seed=11, scale=1.0 / gain)
+        w.q *= gain
+        w.check(w.call())
+    w = World([300], [new], 2, 1, dtype=F32, seed=12)
+    w.cache.scales[..., 1] = 2.0 ** torch.arange(-48, 48, device=DEV)[torch.arange(w.pages, device=DEV) * 13 % 96]
+    w.check(w.call())
+    w.q[:] = 0
+    w.check(w.call())
+    w.q[:, :, :, 3] = float("inf")
+    assert bool(w.call().isnan().all())
+
+
+def test_a_cache_of_more_than_4_gib():
+    pages = 600_000                               # 2.4 GB a plane and head
+    cache = paged.Cache(1, 2, pages)
+    params = paged.Params(1, 2, 2, None, F16)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    q, k, v = torch.randn((3, 1, 100, 2, 64), generator=g, device=DEV).half().unbind(0)
+    out = []
+    for ids in ([pages - 1, pages - 2], [0, 1]):
+        slots = torch.tensor([ids[t // 64] * 64 + t % 64 for t in range(100)], device=DEV)
+        pos = torch.arange(100, dtype=torch.int32, device=DEV)
+        paged.append(params, cache, k, v, slots, pos)
+        out.append(paged.attend(params, cache, q, pos, i32([0, 100]), i32([ids]), i32([100]), 100, 100))
+        out.append(paged.attend(params, cache, q[:, -1:], pos[-1:], i32([0, 1]), i32([ids]), i32([100]), 1, 100))
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3]) and bool(out[0].any())
+    assert torch.equal(cache.k_codes[0, 1, pages - 2], cache.k_codes[0, 1, 1])
+
+
+# --------------------------------------------------------------- together
+def serve(steps, B, L, H, Hkv, dtype, pages, seed, check):
+    """A serving loop with prompts, single tokens, drafts that are taken back and requests that end."""
+    g = np.random.default_rng(seed)
+    tg = torch.Generator(device=DEV).manual_seed(seed)
+    width = 8
+    pool, cache, cs = paged.PagePool(pages), paged.Cache(L, Hkv, pages), tq.rope_table(width * 64)
+    params = paged.Params(L, H, Hkv, cs, dtype)
+    table, seq_len = torch.full((B, width), -1, dtype=torch.int32, device=DEV), i32([0] * B)
+    state = ref.Pool(range(pages - 1, -1, -1), table.tolist(), [0] * B)
+    host = ref.CacheRef(cache)
+    for step in range(steps):
+        new = [int(g.integers(1, 200)) if n == 0 else int(g.choice([1, 1, 1, 4, 70])) for n in state.len]
+        rows = sum(new)
+        slots, pos, row0, granted = paged.assign(pool, table, seq_len, i32(new), rows)
+        w_slots, w_pos, w_row0, w_granted = state.assign(new, rows, pages)
+        assert slots.tolist() == w_slots and granted.tolist() == w_granted
+        x = torch.randn((L, rows, H + 2 * Hkv, 64), generator=tg, device=DEV).to(dtype)
+        q, k, v = x[:, :, :H], x[:, :, H:H + Hkv], x[:, :, H + Hkv:]
+        outs = []
+        for l in range(L):
+            paged.append(params, cache, k[l:l + 1], v[l:l + 1], slots, pos, layer0=l)
+            outs.append(paged.attend(params, cache, q[l:l + 1], pos, row0, table, seq_len, max(new), width * 64, layer0=l))
+        host.append(k.float().cpu().numpy(), v.float().cpu().numpy(), w_slots, w_pos, cs.cpu().numpy(), False)
+        same_cache(cache, host)
+        check(torch.cat(outs), q, host, state, w_pos, w_row0, w_granted, cs)
+        keep = [0 if g.random() < 0.2 else n - int(g.integers(0, 4)) * (g.random() < 0.3) for n in state.len]
+        paged.release(pool, table, seq_len, i32(keep))
+        state.release(keep)
+        check_pool(pool, state, table, seq_len)
+    assert sorted(state.stack + [p for r in state.table for p in r if p >= 0]) == list(range(pages))
+
+
+@pytest.mark.parametrize("dtype,pages", [(F16, 40), (BF16, 14)])
+def test_a_serving_loop(dtype, pages):
+    refused = []
+
+    def check(got, q, host, state, pos, row0, granted, cs):
+        scale = 2.0 ** torch.tensor(host.e, dtype=torch.float64)
+        k = (torch.tensor(host.k) * scale[..., 0, None, None]).to(DEV)
+        v = (torch.tensor(host.v) * scale[..., 1, None, None]).to(DEV)
+        ang = torch.arange(512, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(32, dtype=torch.float64) / 32)
+        z = torch.polar(torch.ones_like(ang), ang).to(DEV)
+        lens = [n if ok else 0 for n, ok in zip(state.len, granted)]
+        p = [max(x, 0) for x in pos]
+        want, spread, size = ref.attend(k, v, q.double(), p, row0, state.table, lens, True, 0.125, z)
+        tol = ref.bound(want, spread, size, max(lens + [1]), 1 if dtype is F16 else 0, dtype)
+        for b, ok in enumerate(granted):
+            a, e = row0[b], row0[b + 1]
+            if ok:
+                assert bool(((got[:, a:e].double() - want[:, a:e]).abs() <= tol[:, a:e]).all())
+            else:
+                refused.append(b)
+                assert bool(got[:, a:e].isnan().all())
+    serve(6, 5, 2, 4, 2, dtype, pages, 21, check)
+    assert bool(refused) == (pages < 20)
+
+
+def test_a_captured_step():
+    """assign, append and attend of a decode step in one graph, replayed between eager work of the same kind."""
+    B, L, H, Hkv, width, pages = 6, 2, 8, 2, 40, 300
+    cs = tq.rope_table(width * 64)
+    params = paged.Params(L, H, Hkv, cs, F16)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    worlds = []
+    for _ in range(2):
+        pool, cache = paged.PagePool(pages), paged.Cache(L, Hkv, pages)
+        table, n = torch.full((B, width), -1, dtype=torch.int32, device=DEV), i32([0] * B)
+        worlds.append((pool, cache, table, n))
+    start = i32([3, 64, 700, 1, 2000, 127])
+    rows = int(start.sum())
+    x = torch.randn((L, rows, H + 2 * Hkv, 64), generator=g, device=DEV).half()
+    steps = torch.randn((5, L, B, H + 2 * Hkv, 64), generator=g, device=DEV).half()
+    ones = torch.ones(B, dtype=torch.int32, device=DEV)
+    need = paged.workspace_bytes(params, L, B, 1, width * 64)
+    assert need > 0
+    ws = torch.zeros(need, dtype=torch.uint8, device=DEV)
+
+    def one(world, x, out, room):
+        pool, cache, table, n = world
+        slots, pos, row0, _ = paged.assign(pool, table, n, ones, B, out=room)
+        paged.append(params, cache, x[:, :, H:H + Hkv], x[:, :, H + Hkv:], slots, pos)
+        return paged.attend(params, cache, x[:, :, :H], pos, row0, table, n, 1, width * 64, out=out, workspace=ws)
+
+    def room():
+        return (torch.empty(B, dtype=torch.int64, device=DEV), i32([0] * B), i32([0] * (B + 1)), i32([0] * B))
+
+    for world in worlds:
+        pool, cache, table, n = world
+        slots, pos, row0, granted = paged.assign(pool, table, n, start, rows)
+        assert granted.tolist() == [1] * B
+        paged.append(params, cache, x[:, :, H:H + Hkv], x[:, :, H + Hkv:], slots, pos)
+    static, out = steps[0].clone(), torch.empty((L, B, H, 64), dtype=F16, device=DEV)
+    captured, eager = worlds
+    room_c, room_e = room(), room()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    saved = [t.clone() for t in (captured[0].stack, captured[0].state, captured[1].k_codes, captured[1].v_codes,
+                                 captured[1].scales, captured[2], captured[3])]
+    with torch.cuda.stream(side):
+        one(captured, static, out, room_c)                # warm up, then put everything back
+    torch.cuda.current_stream().wait_stream(side)
+    for t, was in zip((captured[0].stack, captured[0].state, captured[1].k_codes, captured[1].v_codes,
+                       captured[1].scales, captured[2], captured[3]), saved):
+        t.copy_(was)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one(captured, static, out, room_c)
+    for i in range(5):
+        static.copy_(steps[i])
+        graph.replay()
+        got = out.clone()
+        want = one(eager, steps[i], None, room_e)
+        assert torch.equal(got, want) and torch.equal(captured[2], eager[2]) and torch.equal(captured[3], eager[3])
+        assert torch.equal(captured[1].k_codes, eager[1].k_codes) and torch.equal(captured[1].v_codes, eager[1].v_codes)
+        if i % 2:
+            torch.cuda.synchronize()
+
+
+def test_calls_go_to_the_current_stream():
+    w = World([900, 40], [1, 1], 4, 2, seed=3)
+    fine = w.call()
+    torch.cuda.synchronize()
+    args = dict(pos=i32(w.pos), row0=i32(w.row0), table=i32(w.table), seq_len=i32(w.lens))
+    side = torch.cuda.Stream()
+    q = torch.zeros_like(w.q)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            big = torch.randn(4096, 4096, device=DEV) @ torch.randn(4096, 4096, device=DEV)
+        q.copy_(w.q)
+        got = w.call(q=q, **args)
+    side.synchronize()
+    assert big.shape == (4096, 4096) and torch.equal(got, fine)
+
+
+@pytest.mark.parametrize("case", range(6))
+def test_append_of_runs_in_any_form(case):
+    # the same slot twice, descending slots, a page taken up again after skipped rows, across windows of rows
+    slots = [[64, 64], [70] * 200, list(range(127, 63, -1)), [64, 65, -1, -1, 66, 64] + [-1] * 150 + [80, 81],
+             list(range(64, 128)) * 3 + list(range(192, 200)), [5 * 64 + t for t in (3, 4, 9, 10, 11)] * 30][case]
+    cache = random_cache(1, 2, 6, case)
+    want = ref.CacheRef(cache)
+    g = torch.Generator(device=DEV).manual_seed(case)
+    size = 2.0 ** torch.randint(-9, 6, (1, len(slots), 1, 1), generator=g, device=DEV).float()
+    k, v = (torch.randn((2, 1, len(slots), 2, 64), generator=g, device=DEV) * size).unbind(0)
+    paged.append(paged.Params(1, 2, 2, None, F32), cache, k, v, torch.tensor(slots, device=DEV), i32([0] * len(slots)))
+    want.append(k.cpu().numpy(), v.cpu().numpy(), slots, [0] * len(slots), None, False)
+    same_cache(cache, want)
