@@ -59,7 +59,7 @@ typedef struct tqp_params {
   int32_t io_dtype;          /* TQ_F16, TQ_F32 or TQP_BF16 for q, k, v and out */
   uint32_t flags;            /* TQ_ROPE_HALF, TQ_OUT_FP32                     */
   float softmax_scale;       /* logit = q.k * softmax_scale; <= 0 means 1/8   */
-  int32_t rope_positions;    /* rows of rope_cs                               */
+  int32_t rope_positions;    /* rows of rope_cs, at most 2^23                 */
   const float* rope_cs;      /* device [rope_positions][32][2] (cos, sin) from
                                 tq_rope_table, 16-byte aligned; NULL: q and k
                                 come rotated (or the model has no RoPE)       */
@@ -150,7 +150,8 @@ TQ_API tq_status tqp_release(const tqp_pool* pool, int32_t* table, int32_t table
  * Where rows of another page are between them, what that page holds afterwards
  * is not defined (other pages are not touched).
  *
- *   k, v   device rows [nlayers][rows][kv_heads][64] of io_dtype.
+ *   k, v   device rows [nlayers][rows][kv_heads][64] of io_dtype; their
+ *          row_stride is at most 2^23.
  *   slots  device int64 [rows];  pos device int32 [rows] (unused and may be
  *          NULL without rope_cs).
  */

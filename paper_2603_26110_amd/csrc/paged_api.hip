@@ -33,6 +33,8 @@ tq_status hip_status(hipError_t e, const char* what) {
 }
 
 constexpr int64_t kMaxPages = (int64_t)1 << 24;
+constexpr int32_t kMaxPositions = 1 << 23;   // offsets into the table of cos and sin, and
+constexpr int64_t kMaxRowStride = 1 << 23;   // of 64 rows of k or v, in 32 bits
 
 tq_status check_params(const tqp_params* p, int32_t layer0, int32_t nlayers) {
   if (!p) return fail(TQ_ERR_ARG, "params is NULL");
@@ -47,7 +49,8 @@ tq_status check_params(const tqp_params* p, int32_t layer0, int32_t nlayers) {
   if (!std::isfinite(p->softmax_scale)) return fail(TQ_ERR_ARG, "softmax_scale must be finite");
   if (p->rope_cs) {
     if (!aligned(p->rope_cs, 16)) return fail(TQ_ERR_ALIGN, "rope_cs must be 16-byte aligned");
-    if (p->rope_positions <= 0) return fail(TQ_ERR_ARG, "rope_positions must be positive");
+    if (p->rope_positions <= 0 || p->rope_positions > kMaxPositions)
+      return fail(TQ_ERR_ARG, "rope_positions must be positive and at most 2^23 (got %d)", p->rope_positions);
   }
   if (nlayers < 0) return fail(TQ_ERR_ARG, "nlayers must be >= 0");
   if (layer0 < 0 || (int64_t)layer0 + nlayers > p->num_layers)
@@ -143,6 +146,8 @@ tq_status tqp_append(const tqp_params* params, const tqp_cache* cache, const tqp
   if (rows < 0) return fail(TQ_ERR_ARG, "rows must be >= 0");
   if (rows == 0 || nlayers == 0) return ok();
   if ((s = check_rows(k, "k")) != TQ_OK || (s = check_rows(v, "v")) != TQ_OK) return s;
+  if (k->row_stride < 0 || k->row_stride > kMaxRowStride || v->row_stride < 0 || v->row_stride > kMaxRowStride)
+    return fail(TQ_ERR_ARG, "k and v: row strides must be in [0, 2^23]");
   if (!slots || (params->rope_cs && !pos)) return fail(TQ_ERR_ARG, "a required pointer is NULL");
   if (((int64_t)rows + 63) / 64 * nlayers * params->kv_heads >= ((int64_t)1 << 30))
     return fail(TQ_ERR_ARG, "too many token-heads for one call");

@@ -2,15 +2,20 @@
 //
 // A page's scale covers all its tokens of one head, so the unit of work is a
 // run: consecutive rows whose slots follow each other within one page. One
-// wave takes one run for one (layer, head), holds the run's keys and values in
-// registers, and is the only writer of that page: runs of one page that come
-// one after the other are one wave's, in their order. Waves find the pages that
-// start in a window of 64 rows from the rows' slots (ballots); the pages of
-// a window are shared by `share` waves, more where there are few windows.
+// block takes a run for one (layer, head) and is the only writer of that page;
+// runs of one page that come one after the other are one block's, in their
+// order. Waves find the runs of a window of 64 rows from the rows' slots, with
+// ballots, so that a call needs nothing but slots.
 //
-// Bound by memory (per token and head 256 bytes of fp16 in, 128 out): a run of
-// many tokens loads all its rows before it uses any. A run of few tokens takes
-// a path with a dimension per lane that writes only its own bytes.
+// The two shapes of a call want different waves, and which one it is only the
+// device knows. So the first part of the grid takes the runs of several tokens
+// (prompts: a block's four waves have a half of the run's keys or values each
+// in their registers), the second the runs of one token (decode steps: four
+// (token, head)s per wave at a time, 16 lanes each); the part that finds nothing
+// in its windows ends after the ballots. (One wave with a whole run took 223
+// registers, so that few waves could wait for memory at once.)
+//
+// Bound by memory: 256 bytes of fp16 in and 128 out per token and head.
 #include <algorithm>
 
 #include "paged_device.hpp"
@@ -18,14 +23,24 @@
 namespace tqp {
 namespace {
 
-constexpr int kFew = 4;          // tokens of a run that takes the path of a dimension per lane
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+enum Rope { kNone = 0, kPairs = 1, kHalf = 2 };   // pairs (2m, 2m+1) or (m, m+32)
+constexpr int kFew = 4;          // tokens of a run that is taken token by token
 
-struct Unit {
-  int l, h, page, at, row, count;   // tokens [at, at + count) of the page, from this row on
+// The grid's two parts: blocks per (window, layer, head) and per (window, layer).
+struct Grid {
+  int windows, share, singles, blocks_runs, blocks;
 };
 
-// Both positions' cos and sin applied in binary32, products and sum rounded
-// on their own (this file is compiled without contraction).
+struct Run {
+  int l, h, at, row, count;      // tokens [at, at + count) of the page, from this row on
+  uint8_t* k;
+  uint8_t* v;
+  float2* scales;
+};
+
+// Both values of a pair rotated in binary32, products and sum rounded on their
+// own (this file is compiled without contraction).
 __device__ __forceinline__ void rotate(float& a, float& b, float c, float s) {
   const float x = a * c - b * s, y = a * s + b * c;
   a = x;
@@ -46,11 +61,11 @@ __device__ __forceinline__ Scale new_scale(uint32_t amax, float old, bool fresh)
   s.grown = !fresh && s.e > was;
   if (!fresh) s.e = max(s.e, was);
   s.inv = pow2(-s.e);
-  s.move = s.grown ? pow2(max(was - s.e, -126)) : 1.0f;
+  s.move = s.grown ? pow2(was - s.e) : 1.0f;
   return s;
 }
 
-// Everything the page holds moved to the new scale (rare: its largest value
+// Everything a page holds moved to a new scale (rare: its largest value
 // crossed a power of two). The stores are complete when this returns, so that
 // the new tokens' may follow.
 __device__ void move_page(uint8_t* plane, float by, int lane) {
@@ -65,98 +80,133 @@ __device__ void move_page(uint8_t* plane, float by, int lane) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// A run of at most kFew tokens: lane d has dimension d of each token.
-template <int IO>
-__device__ void append_few(const AppendArgs& a, const Unit& u, uint8_t* kp, uint8_t* vp, float* scales, int lane) {
-  float k[kFew], v[kFew];
-  const int64_t kb = u.l * a.k.layer + u.h * a.k.head + lane, vb = u.l * a.v.layer + u.h * a.v.head + lane;
-#pragma unroll
-  for (int j = 0; j < kFew; ++j) {
-    const int64_t row = u.row + min(j, u.count - 1);
-    k[j] = load_element<IO>(a.k.data, kb + row * a.k.row);
-    v[j] = load_element<IO>(a.v.data, vb + row * a.v.row);
-  }
-  const float2 old = *reinterpret_cast<const float2*>(scales);
-  if (a.cs) {
-    const int pair = a.rope_half ? lane & 31 : lane >> 1, with = a.rope_half ? 32 : 1;
-    const bool second = (lane & with) != 0;
-#pragma unroll
-    for (int j = 0; j < kFew; ++j) {
-      const int pos = a.pos[u.row + min(j, u.count - 1)];
-      const float2 cs = reinterpret_cast<const float2*>(a.cs)[(int64_t)pos * (kDim / 2) + pair];
-      const float o = __shfl_xor(k[j], with, 64);
-      float x = second ? o : k[j], y = second ? k[j] : o;
-      rotate(x, y, cs.x, cs.y);
-      k[j] = second ? y : x;
-    }
-  }
-  uint32_t km = 0, vm = 0, bad = 0;
-#pragma unroll
-  for (int j = 0; j < kFew; ++j) {
-    const uint32_t kj = abs_bits(k[j]), vj = abs_bits(v[j]);
-    if (__any(max(kj, vj) >= kInfBits)) {
-      bad |= 1u << j;
-    } else {
-      km = max(km, kj);
-      vm = max(vm, vj);
-    }
-  }
-  const bool fresh = u.at == 0;
-  const Scale ks = new_scale(wave_max_bits(km), old.x, fresh), vs = new_scale(wave_max_bits(vm), old.y, fresh);
-  if (ks.grown) move_page(kp, ks.move, lane);
-  if (vs.grown) move_page(vp, vs.move, lane);
-#pragma unroll
-  for (int j = 0; j < kFew; ++j) {
-    if (j >= u.count) break;
-    const int t = u.at + j;
-    const uint32_t w = codes4(k[j] * ks.inv, v[j] * vs.inv, 0.0f, 0.0f);
-    const bool b = (bad >> j) & 1;
-    kp[t * kDim + lane] = b ? 0x7F : (uint8_t)(w & 0xFF);
-    vp[((t >> 2) & 3) * 1024 + lane * 16 + ((t >> 4) << 2) + (t & 3)] = b ? 0 : (uint8_t)((w >> 8) & 0xFF);
-  }
-  if (lane == 0 && (fresh || ks.grown || vs.grown))
-    *reinterpret_cast<float2*>(scales) = make_float2(pow2(ks.e), pow2(vs.e));
+// Values that all lanes have, as scalars.
+__device__ __forceinline__ uint32_t wave_max_uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(wave_max_bits(v)); }
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
+__device__ __forceinline__ float2 uniform(float2 x) { return make_float2(uniform(x.x), uniform(x.y)); }
+
+__device__ __forceinline__ int value_byte(int t, int d) {
+  return ((t >> 2) & 3) * 1024 + d * 16 + ((t >> 4) << 2) + (t & 3);
 }
 
-// A run of any length, all of it in registers.
-//   keys:   lane has dimensions [d0, d0+4) and [d1, d1+4) of tokens 8 m + lane/8
-//           of the page (the two fours hold whole RoPE pairs)
-//   values: lane has dimensions 4 (lane%16) .. +3 of the tokens 16 i + 4 (lane/16) + r,
-//           which is how a value plane's 16-byte pieces hold them
-template <int IO>
-__device__ void append_many(const AppendArgs& a, const Unit& u, uint8_t* kp, uint8_t* vp, float* scales, int lane) {
-  const int end = u.at + u.count;
+// ------------------------------------------------------- token by token
+// A run of few tokens, or one that holds an infinity or NaN: lane d has
+// dimension d of one token after the other, once for the scales and once for
+// the codes.
+template <int IO, int ROPE>
+__device__ __forceinline__ void append_tokens(const AppendArgs& a, const Run& u, int lane) {
+  const int pair = ROPE == kHalf ? lane & 31 : lane >> 1, with = ROPE == kHalf ? 32 : 1;
+  const bool second = (lane & with) != 0;
+  const int64_t kb = u.l * a.k.layer + u.h * a.k.head + lane, vb = u.l * a.v.layer + u.h * a.v.head + lane;
+  auto load = [&](int j, float& k, float& v) {
+    const int64_t row = u.row + j;
+    k = load_element<IO>(a.k.data, kb + row * a.k.row);
+    v = load_element<IO>(a.v.data, vb + row * a.v.row);
+    if (ROPE != kNone) {
+      const float2 cs = reinterpret_cast<const float2*>(a.cs)[(int64_t)a.pos[row] * (kDim / 2) + pair];
+      const float o = __shfl_xor(k, with, 64);
+      float x = second ? o : k, y = second ? k : o;
+      rotate(x, y, cs.x, cs.y);
+      k = second ? y : x;
+    }
+    return __any(max(abs_bits(k), abs_bits(v)) >= kInfBits) != 0;
+  };
+  const float2 old = uniform(*u.scales);
+  uint32_t km = 0, vm = 0;
+  for (int j = 0; j < u.count; ++j) {
+    float k, v;
+    if (load(j, k, v)) continue;
+    km = max(km, abs_bits(k));
+    vm = max(vm, abs_bits(v));
+  }
   const bool fresh = u.at == 0;
-  float k[8][8], v[16][4];
-  const int d0 = a.rope_half ? 4 * (lane & 7) : 8 * (lane & 7), d1 = d0 + (a.rope_half ? 32 : 4);
-  const int64_t kb = u.l * a.k.layer + u.h * a.k.head, vb = u.l * a.v.layer + u.h * a.v.head + 4 * (lane & 15);
-  const int g = lane >> 4;
+  const Scale ks = new_scale(wave_max_uniform(km), old.x, fresh), vs = new_scale(wave_max_uniform(vm), old.y, fresh);
+  if (ks.grown) move_page(u.k, ks.move, lane);
+  if (vs.grown) move_page(u.v, vs.move, lane);
+  for (int j = 0; j < u.count; ++j) {
+    float k, v;
+    const bool bad = load(j, k, v);
+    const uint32_t w = codes4(k * ks.inv, v * vs.inv, 0.0f, 0.0f);
+    u.k[(u.at + j) * kDim + lane] = bad ? 0x7F : (uint8_t)(w & 0xFF);
+    u.v[value_byte(u.at + j, lane)] = bad ? 0 : (uint8_t)((w >> 8) & 0xFF);
+  }
+  if (lane == 0) *u.scales = make_float2(pow2(ks.e), pow2(vs.e));
+}
+
+// ------------------------------------------------------- a run at a time
+// N elements (4 or 2) as they are in memory.
+template <int IO, int N>
+struct Raw {
+  uint32_t w[IO == kF32 ? N : N / 2];
+};
+
+// (a uniform base and 32 bits of offset, in elements: no address takes registers of its own)
+template <int IO, int N>
+__device__ __forceinline__ Raw<IO, N> load_raw(const uint8_t* base, uint32_t at) {
+  constexpr int kWords = IO == kF32 ? N : N / 2;
+  Raw<IO, N> r;
+  const uint8_t* p = base + at * (uint32_t)io_bytes<IO>();
+  if constexpr (kWords == 1) {
+    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 2) {
+      const u32x2 x = reinterpret_cast<const u32x2*>(p)[i / 2];
+      r.w[i] = x[0];
+      r.w[i + 1] = x[1];
+    }
+  }
+  return r;
+}
+
+template <int IO, int N>
+__device__ __forceinline__ float element(const Raw<IO, N>& f, int j) {
+  if constexpr (IO == kF32) return __uint_as_float(f.w[j]);
+  const uint32_t bits = (f.w[j >> 1] >> (16 * (j & 1))) & 0xFFFFu;
+  if constexpr (IO == kBF16) return __uint_as_float(bits << 16);
+  return __half2float(__ushort_as_half((unsigned short)bits));
+}
+
+// Keys of tokens 32 half .. +31: lane has dimensions [d0, d0+4) and [d1, d1+4)
+// of tokens 32 half + 8 m + lane/8 (the two fours hold whole RoPE pairs). All
+// loads are requested before any is used. top(x) gives the largest of the
+// block's keys, or kInfBits where the run holds what is no number: nothing is
+// written then.
+template <int IO, int ROPE, class Top>
+__device__ __forceinline__ void run_keys(const AppendArgs& a, const Run& u, int half, int lane, Top top) {
+  const int end = u.at + u.count, last = end - 1, first = 32 * half + (lane >> 3);
+  const int d0 = ROPE == kHalf ? 4 * (lane & 7) : 8 * (lane & 7), d1 = d0 + (ROPE == kHalf ? 32 : 4);
+  const int64_t r0 = u.row - u.at;   // the row that the page's first token would have
+  const uint8_t* kb = reinterpret_cast<const uint8_t*>(a.k.data) + (u.l * a.k.layer + u.h * a.k.head + r0 * a.k.row) * io_bytes<IO>();
   // (tokens outside the run take the row of one inside, so that every load is
   // in bounds and none waits on a branch; they change no maximum)
+  auto inside = [&](int m) { return (uint32_t)min(max(first + 8 * m, u.at), last); };
+  uint32_t pos[4];               // (asked for first: the loads of cos and sin wait for them)
 #pragma unroll
-  for (int m = 0; m < 8; ++m) {
-    const int t = min(max(8 * m + (lane >> 3), u.at), end - 1);
-    const int64_t at = kb + (int64_t)(u.row + t - u.at) * a.k.row;
-    float lo[4], hi[4];
-    load_elements<IO>(a.k.data, at + d0, lo);
-    load_elements<IO>(a.k.data, at + d1, hi);
+  for (int m = 0; m < 4; ++m) pos[m] = ROPE != kNone ? (uint32_t)(a.pos + r0)[inside(m)] : 0;
+  Raw<IO, 4> kr[4][2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) { k[m][j] = lo[j]; k[m][4 + j] = hi[j]; }
+  for (int m = 0; m < 4; ++m) {
+    const uint32_t at = inside(m) * (uint32_t)a.k.row;
+    kr[m][0] = load_raw<IO, 4>(kb, at + d0);
+    kr[m][1] = load_raw<IO, 4>(kb, at + d1);
   }
+  const float old = uniform(u.scales->x);
+  float k[4][8];
+  uint32_t km = 0;
+  const int pair = ROPE == kHalf ? d0 : d0 >> 1;
 #pragma unroll
-  for (int n = 0; n < 16; ++n) {
-    const int t = min(max(16 * (n >> 2) + 4 * g + (n & 3), u.at), end - 1);
-    load_elements<IO>(a.v.data, vb + (int64_t)(u.row + t - u.at) * a.v.row, v[n]);
-  }
-  const float2 old = *reinterpret_cast<const float2*>(scales);
-  if (a.cs) {
-    const int pair = a.rope_half ? d0 : d0 >> 1;
+  for (int m = 0; m < 4; ++m) {
 #pragma unroll
-    for (int m = 0; m < 8; ++m) {
-      const int t = min(max(8 * m + (lane >> 3), u.at), end - 1);
-      const float4* cs = reinterpret_cast<const float4*>(a.cs + ((int64_t)a.pos[u.row + t - u.at] * (kDim / 2) + pair) * 2);
+    for (int j = 0; j < 4; ++j) {
+      k[m][j] = element(kr[m][0], j);
+      k[m][4 + j] = element(kr[m][1], j);
+    }
+    if (ROPE != kNone) {
+      const float4* cs = reinterpret_cast<const float4*>(reinterpret_cast<const uint8_t*>(a.cs) + pos[m] * (kDim * 4u) + pair * 8u);
       const float4 c0 = cs[0], c1 = cs[1];
-      if (a.rope_half) {
+      if (ROPE == kHalf) {
         rotate(k[m][0], k[m][4], c0.x, c0.y);
         rotate(k[m][1], k[m][5], c0.z, c0.w);
         rotate(k[m][2], k[m][6], c1.x, c1.y);
@@ -168,74 +218,27 @@ __device__ void append_many(const AppendArgs& a, const Unit& u, uint8_t* kp, uin
         rotate(k[m][6], k[m][7], c1.z, c1.w);
       }
     }
-  }
-  uint32_t km = 0, vm = 0;
-#pragma unroll
-  for (int m = 0; m < 8; ++m)
 #pragma unroll
     for (int j = 0; j < 8; ++j) km = max(km, abs_bits(k[m][j]));
-#pragma unroll
-  for (int n = 0; n < 16; ++n)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) vm = max(vm, abs_bits(v[n][j]));
-  uint64_t bad = 0;              // tokens of the page that hold an infinity or NaN
-  if (__any(max(km, vm) >= kInfBits)) {
-    km = vm = 0;
-#pragma unroll
-    for (int m = 0; m < 8; ++m) {
-      bool b = false;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) b |= abs_bits(k[m][j]) >= kInfBits;
-      const uint64_t lanes = __ballot(b);
-      for (int r = 0; r < 8; ++r)
-        if ((lanes >> (8 * r)) & 0xFF) bad |= 1ull << (8 * m + r);
-    }
-#pragma unroll
-    for (int n = 0; n < 16; ++n) {
-      bool b = false;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) b |= abs_bits(v[n][j]) >= kInfBits;
-      const uint64_t lanes = __ballot(b);
-      for (int r = 0; r < 4; ++r)
-        if ((lanes >> (16 * r)) & 0xFFFF) bad |= 1ull << (16 * (n >> 2) + 4 * r + (n & 3));
-    }
-#pragma unroll
-    for (int m = 0; m < 8; ++m) {
-      const bool b = (bad >> min(max(8 * m + (lane >> 3), u.at), end - 1)) & 1;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (b) k[m][j] = 0.0f;
-        km = max(km, abs_bits(k[m][j]));
-      }
-    }
-#pragma unroll
-    for (int n = 0; n < 16; ++n) {
-      const bool b = (bad >> min(max(16 * (n >> 2) + 4 * g + (n & 3), u.at), end - 1)) & 1;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (b) v[n][j] = 0.0f;
-        vm = max(vm, abs_bits(v[n][j]));
-      }
-    }
   }
-  const Scale ks = new_scale(wave_max_bits(km), old.x, fresh), vs = new_scale(wave_max_bits(vm), old.y, fresh);
+  km = top(wave_max_uniform(km));
+  if (km >= kInfBits) return;
+  const Scale s = new_scale(km, old, u.at == 0);
 #pragma unroll
-  for (int m = 0; m < 8; ++m) {
-    const int t = 8 * m + (lane >> 3);
+  for (int m = 0; m < 4; ++m) {
+    const int t = first + 8 * m;
     const bool mine = t >= u.at && t < end;
-    uint32_t* p0 = reinterpret_cast<uint32_t*>(kp + t * kDim + d0);
-    uint32_t* p1 = reinterpret_cast<uint32_t*>(kp + t * kDim + d1);
-    uint32_t w0, w1;
-    if (mine) {
-      w0 = codes4(k[m][0] * ks.inv, k[m][1] * ks.inv, k[m][2] * ks.inv, k[m][3] * ks.inv);
-      w1 = codes4(k[m][4] * ks.inv, k[m][5] * ks.inv, k[m][6] * ks.inv, k[m][7] * ks.inv);
-      if ((bad >> t) & 1) w0 = w1 = 0x7F7F7F7Fu;
-    } else if (ks.grown) {
-      w0 = rescale4(*p0, ks.move);
-      w1 = rescale4(*p1, ks.move);
+    uint32_t* p0 = reinterpret_cast<uint32_t*>(u.k + (uint32_t)(t * kDim + d0));
+    uint32_t* p1 = reinterpret_cast<uint32_t*>(u.k + (uint32_t)(t * kDim + d1));
+    uint32_t w0 = codes4(k[m][0] * s.inv, k[m][1] * s.inv, k[m][2] * s.inv, k[m][3] * s.inv);
+    uint32_t w1 = codes4(k[m][4] * s.inv, k[m][5] * s.inv, k[m][6] * s.inv, k[m][7] * s.inv);
+    if (s.grown) {               // (uniform)
+      const uint32_t o0 = rescale4(*p0, s.move), o1 = rescale4(*p1, s.move);
+      w0 = mine ? w0 : o0;
+      w1 = mine ? w1 : o1;
     }
-    if (mine || ks.grown) {
-      if (a.rope_half) {
+    if (mine || s.grown) {
+      if (ROPE == kHalf) {
         *p0 = w0;
         *p1 = w1;
       } else {
@@ -243,42 +246,70 @@ __device__ void append_many(const AppendArgs& a, const Unit& u, uint8_t* kp, uin
       }
     }
   }
-  uint32_t mine[4];              // bytes of the run's tokens, per word of a piece
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    mine[i] = 0;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = 16 * i + 4 * g + r;
-      if (t >= u.at && t < end) mine[i] |= 0xFFu << (8 * r);
-    }
-  }
-  const bool whole = u.count == kPage;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    u32x4* p = reinterpret_cast<u32x4*>(vp + g * 1024 + (4 * (lane & 15) + j) * 16);
-    u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = codes4(v[4 * i][j] * vs.inv, v[4 * i + 1][j] * vs.inv, v[4 * i + 2][j] * vs.inv, v[4 * i + 3][j] * vs.inv);
-    if (!whole) {
-      const u32x4 was = *p;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t kept = vs.grown ? rescale4(was[i], vs.move) : was[i];
-        w[i] = (w[i] & mine[i]) | (kept & ~mine[i]);
-      }
-    }
-    *p = w;
-  }
-  if (lane == 0) *reinterpret_cast<float2*>(scales) = make_float2(pow2(ks.e), pow2(vs.e));
+  if (half == 0 && lane == 0) u.scales->x = pow2(s.e);
 }
 
-__device__ __forceinline__ int first_bit(uint64_t m) { return __ffsll((unsigned long long)m) - 1; }
+// Values of the token groups 2 half and 2 half + 1 of the page: lane has
+// dimensions 2 (lane%32) and the next of tokens 16 i + 4 g + r, g = 2 half +
+// lane/32, which is how a value plane's 16-byte pieces hold them.
+template <int IO, class Top>
+__device__ __forceinline__ void run_values(const AppendArgs& a, const Run& u, int half, int lane, Top top) {
+  const int end = u.at + u.count, last = end - 1, g = 2 * half + (lane >> 5), d = 2 * (lane & 31);
+  const int64_t r0 = u.row - u.at;
+  const uint8_t* vb = reinterpret_cast<const uint8_t*>(a.v.data) + (u.l * a.v.layer + u.h * a.v.head + r0 * a.v.row) * io_bytes<IO>();
+  Raw<IO, 2> vr[16];
+#pragma unroll
+  for (int n = 0; n < 16; ++n) {
+    const uint32_t t = (uint32_t)min(max(16 * (n >> 2) + 4 * g + (n & 3), u.at), last);
+    vr[n] = load_raw<IO, 2>(vb, t * (uint32_t)a.v.row + d);
+  }
+  const float old = uniform(u.scales->y);
+  u32x4* vp = reinterpret_cast<u32x4*>(u.v + (uint32_t)(g * 1024 + d * 16));
+  u32x4 was[2];
+  if (u.count < kPage) {         // (pieces that hold other tokens, too)
+    was[0] = vp[0];
+    was[1] = vp[1];
+  }
+  uint32_t vm = 0;
+#pragma unroll
+  for (int n = 0; n < 16; ++n) vm = max(vm, max(abs_bits(element(vr[n], 0)), abs_bits(element(vr[n], 1))));
+  vm = top(wave_max_uniform(vm));
+  if (vm >= kInfBits) return;
+  const Scale s = new_scale(vm, old, u.at == 0);
+  u32x4 w[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[j][i] = codes4(element(vr[4 * i], j) * s.inv, element(vr[4 * i + 1], j) * s.inv, element(vr[4 * i + 2], j) * s.inv,
+                       element(vr[4 * i + 3], j) * s.inv);
+  if (u.count < kPage) {
+    // the other tokens' bytes stay, or move to the new scale
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t mine = 0;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * i + 4 * g + r;
+        if (t >= u.at && t < end) mine |= 0xFFu << (8 * r);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t kept = s.grown ? rescale4(was[j][i], s.move) : was[j][i];
+        w[j][i] = (w[j][i] & mine) | (kept & ~mine);
+      }
+    }
+  }
+  vp[0] = w[0];
+  vp[1] = w[1];
+  if (half == 0 && lane == 0) u.scales->y = pow2(s.e);
+}
 
+// ------------------------------------------------------------ the windows
+__device__ __forceinline__ int first_bit(uint64_t m) { return __ffsll((unsigned long long)m) - 1; }
 __device__ __forceinline__ int last_bit(uint64_t m) { return 63 - __clzll((long long)m); }
 
-// x of a lane, the same for all (i uniform) or each lane's own choice.
+// x of one lane for all (i uniform, a scalar), or of each lane's own choice.
 __device__ __forceinline__ int64_t broadcast(int64_t x, int i) {
   const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, i);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)x >> 32), i);
@@ -286,141 +317,308 @@ __device__ __forceinline__ int64_t broadcast(int64_t x, int i) {
 }
 __device__ __forceinline__ int64_t shuffled(int64_t x, int i) { return __shfl(x, i, 64); }
 
-template <int IO>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a, int windows, int share, int waves) {
-  const int lane = threadIdx.x & 63;
-  const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (id >= waves) return;
-  // (heads innermost: the waves of a block read the same rows of cos and sin)
-  const int h = id % a.heads, line = id / a.heads;
-  const int s = line % share, rest = line / share;
-  const int w = rest % windows, l = rest / windows;
-  const int t0 = w * 64;
-  const int64_t limit = (int64_t)a.cache.pages * kPage;
-  // slot of a row, -1 where the row is skipped or not there
-  auto slot_of = [&](int64_t t) {
-    if (t < 0 || t >= a.rows) return (int64_t)-1;
-    const int64_t slot = a.slots[t];
-    bool ok = slot >= 0 && slot < limit;
-    if (a.cs) {
-      const int pos = a.pos[t];
-      ok = ok && pos >= 0 && pos < a.rope_positions;
-    }
-    return ok ? slot : (int64_t)-1;
-  };
-  const int64_t s0 = slot_of((int64_t)t0 + lane), s1 = slot_of((int64_t)t0 + 64 + lane);
-  const uint64_t v0 = __ballot(s0 >= 0), v1 = __ballot(s1 >= 0);
-  if (!v0) return;
+// What decides a row's slot (-1 where the row is skipped or not there), loaded
+// without a branch so that several rows' loads are on their way at once.
+struct Place {
+  int64_t slot;
+  int pos;
+};
+
+__device__ __forceinline__ Place load_place(const AppendArgs& a, int64_t t) {
+  const int64_t i = min(max(t, (int64_t)0), (int64_t)a.rows - 1);
+  return Place{a.slots[i], a.cs ? a.pos[i] : 0};
+}
+
+__device__ __forceinline__ int64_t slot_at(const AppendArgs& a, int64_t t, Place p) {
+  const bool ok = (t >= 0) & (t < a.rows) & (p.slot >= 0) & (p.slot < (int64_t)a.cache.pages * kPage) &
+                  (!a.cs | ((p.pos >= 0) & (p.pos < a.rope_positions)));
+  return ok ? p.slot : -1;
+}
+
+__device__ __forceinline__ int64_t slot_of(const AppendArgs& a, int64_t t) { return slot_at(a, t, load_place(a, t)); }
+
+// A window of 64 rows and the next, as masks of rows: those that are there;
+// those that continue the run of the row before; those that are the first of a
+// page that the row before them (of those that are there) does not have.
+struct Window {
+  int t0;
+  int64_t s0, s1;                // this lane's slots
+  uint64_t v0, v1, f0, f1, lead0, lead1;
+};
+
+__device__ __forceinline__ Window window_of(const AppendArgs& a, int w, int lane) {
+  Window x;
+  x.t0 = w * 64;
+  const int64_t t = (int64_t)x.t0 + lane, tb = (int64_t)x.t0 - 1 - lane;
+  const Place p = load_place(a, t), q = load_place(a, t + 64), o = load_place(a, tb);
+  x.s0 = slot_at(a, t, p);
+  x.s1 = slot_at(a, t + 64, q);
+  int64_t before = slot_at(a, tb, o);
+  x.v0 = __ballot(x.s0 >= 0);
+  x.v1 = __ballot(x.s1 >= 0);
+  x.f0 = x.f1 = x.lead0 = x.lead1 = 0;
+  if (!x.v0) return x;
   // the last slot before the window (rows that are skipped do not count)
   int64_t carry = -1;
-  bool beside = false;           // it is that of the row before
-  for (int64_t t = t0; t > 0 && carry < 0; t -= 64) {
-    const int64_t x = slot_of(t - 1 - lane);
-    const uint64_t there = __ballot(x >= 0);
-    if (there) carry = shuffled(x, first_bit(there));
-    if (t == t0) beside = there & 1;
+  const bool beside = __ballot(before >= 0) & 1;   // it is that of the row before
+  for (int64_t first = x.t0; first > 0; first -= 64) {
+    const uint64_t there = __ballot(before >= 0);
+    if (there) {
+      carry = broadcast(before, first_bit(there));
+      break;
+    }
+    before = slot_of(a, first - 65 - lane);
   }
-  // The slot before each row's own. A row whose page is that of the slot before
-  // is chained to it; if it also has the next slot, and no row is skipped
-  // between, it belongs to the same run.
   const uint64_t lower = (1ull << lane) - 1;
-  const int64_t last = shuffled(s0, last_bit(v0));
-  const int64_t p0 = shuffled(s0, last_bit((v0 & lower) | 1)), p1 = shuffled(s1, last_bit((v1 & lower) | 1));
-  const int64_t before0 = v0 & lower ? p0 : carry, before1 = v1 & lower ? p1 : last;
-  const bool chained0 = s0 >= 0 && before0 >= 0 && s0 / kPage == before0 / kPage;
-  const bool chained1 = s1 >= 0 && s1 / kPage == before1 / kPage;
-  const uint64_t b0 = v0 << 1 | (beside ? 1 : 0), b1 = v1 << 1 | v0 >> 63;
-  const uint64_t f0 = __ballot(chained0 && ((b0 >> lane) & 1) && s0 == before0 + 1);
-  const uint64_t f1 = __ballot(chained1 && ((b1 >> lane) & 1) && s1 == before1 + 1);
-  const uint64_t lead0 = __ballot(s0 >= 0 && !chained0), lead1 = __ballot(s1 >= 0 && !chained1);
+  const int64_t last = broadcast(x.s0, last_bit(x.v0));
+  const int64_t n0 = shuffled(x.s0, last_bit((x.v0 & lower) | 1)), n1 = shuffled(x.s1, last_bit((x.v1 & lower) | 1));
+  const int64_t before0 = x.v0 & lower ? n0 : carry, before1 = x.v1 & lower ? n1 : last;
+  const bool chained0 = x.s0 >= 0 && before0 >= 0 && x.s0 / kPage == before0 / kPage;
+  const bool chained1 = x.s1 >= 0 && x.s1 / kPage == before1 / kPage;
+  const uint64_t b0 = x.v0 << 1 | (beside ? 1 : 0), b1 = x.v1 << 1 | x.v0 >> 63;
+  x.f0 = __ballot(chained0 && ((b0 >> lane) & 1) && x.s0 == before0 + 1);
+  x.f1 = __ballot(chained1 && ((b1 >> lane) & 1) && x.s1 == before1 + 1);
+  x.lead0 = __ballot(x.s0 >= 0 && !chained0);
+  x.lead1 = __ballot(x.s1 >= 0 && !chained1);
+  return x;
+}
 
-  // This wave's share of the pages that start in the window, each with all of
-  // its runs in the order of the rows (tqp_assign gives one run a page).
-  uint64_t todo = lead0;
+// The pages that start in the window and take one token: the next row that is
+// there has another page. (Without one in the two windows the page counts as
+// taking more, which is as right.)
+__device__ __forceinline__ uint64_t single_rows(const Window& x, int lane) {
+  const uint64_t above = lane == 63 ? 0 : x.v0 >> (lane + 1) << (lane + 1);
+  const bool alone = above ? (x.lead0 >> first_bit(above)) & 1 : x.v1 ? (x.lead1 >> first_bit(x.v1)) & 1 : true;
+  return __ballot(((x.lead0 >> lane) & 1) && alone);
+}
+
+// ------------------------------------------------- runs of several tokens
+template <int IO, int ROPE>
+__device__ __forceinline__ void take_runs(const AppendArgs& a, const Grid& gr, int id, int lane) {
+  __shared__ uint32_t s_top[2][kWaves];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int turn = 0;
+  const int h = id % a.heads, line = id / a.heads;
+  const int s = line % gr.share, rest = line / gr.share;
+  const int l = rest / gr.windows;
+  const Window x = window_of(a, rest - l * gr.windows, lane);
+  uint64_t todo = x.lead0 & ~single_rows(x, lane);
   for (int n = 0; todo; ++n) {
     int i = first_bit(todo);
     todo &= todo - 1;
-    if (n % share != s) continue;
-    int64_t row, slot = broadcast(s0, i);
-    int count;
-    bool covered = true;         // by the two windows' masks
-    Unit u;
+    if (n % gr.share != s) continue;
+    int64_t row, slot = broadcast(x.s0, i);
+    const int page = (int)(slot / kPage);
+    const int64_t region = ((int64_t)(a.layer0 + l) * a.heads + h) * a.cache.pages + page;
+    Run u;
     u.l = l;
     u.h = h;
-    u.page = (int)(slot / kPage);
-    const int64_t region = ((int64_t)(a.layer0 + l) * a.heads + h) * a.cache.pages + u.page;
+    u.k = a.cache.k + region * kPageBytes;
+    u.v = a.cache.v + region * kPageBytes;
+    u.scales = reinterpret_cast<float2*>(a.cache.scales) + region;
+    bool covered = true;         // by the two windows' masks
     while (true) {
       if (covered) {
         // rows that follow row i: the ones after bit i of f0, then of f1
-        const uint64_t after = i == 63 ? f1 : (f0 >> (i + 1)) | (f1 << (63 - i));
-        row = (int64_t)t0 + i;
-        count = min(after == ~0ull ? 64 : first_bit(~after), 63) + 1;
+        const uint64_t after = i == 63 ? x.f1 : (x.f0 >> (i + 1)) | (x.f1 << (63 - i));
+        row = (int64_t)x.t0 + i;
+        u.count = min(after == ~0ull ? 64 : first_bit(~after), 63) + 1;
       } else {
-        const uint64_t on = __ballot(slot_of(row + lane) == slot + lane && slot % kPage + lane < kPage);
-        count = on == ~0ull ? 64 : first_bit(~on);
+        const uint64_t on = __ballot(slot_of(a, row + lane) == slot + lane && slot % kPage + lane < kPage);
+        u.count = on == ~0ull ? 64 : first_bit(~on);
       }
       u.at = (int)(slot % kPage);
       u.row = (int)row;
-      u.count = count;
-      uint8_t* kp = a.cache.k + region * kPageBytes;
-      uint8_t* vp = a.cache.v + region * kPageBytes;
-      if (count <= kFew)
-        append_few<IO>(a, u, kp, vp, a.cache.scales + region * 2, lane);
-      else
-        append_many<IO>(a, u, kp, vp, a.cache.scales + region * 2, lane);
+      bool whole = u.count > kFew;
+      if (whole) {
+        // All waves come here for every run, and what one run leaves in LDS is
+        // read before the run after the next writes there.
+        turn ^= 1;
+        auto top = [&](uint32_t x) {
+          if (lane == 0) s_top[turn][wave] = x;
+          __syncthreads();
+          const uint32_t k = max(s_top[turn][0], s_top[turn][1]), v = max(s_top[turn][2], s_top[turn][3]);
+          whole = max(k, v) < kInfBits;
+          return uniform(whole ? (wave < 2 ? k : v) : kInfBits);
+        };
+        if (wave < 2)
+          run_keys<IO, ROPE>(a, u, wave, lane, top);
+        else
+          run_values<IO>(a, u, wave - 2, lane, top);
+      }
+      if (!whole && wave == 0) append_tokens<IO, ROPE>(a, u, lane);
       // the next row that is there: another page's, or another run of this one
       if (covered) {
-        i += count;
-        const uint64_t more0 = i < 64 ? v0 >> i << i : 0;
-        const uint64_t more1 = i <= 64 ? v1 : i < 128 ? v1 >> (i - 64) << (i - 64) : 0;
+        i += u.count;
+        const uint64_t more0 = i < 64 ? x.v0 >> i << i : 0;
+        const uint64_t more1 = i <= 64 ? x.v1 : i < 128 ? x.v1 >> (i - 64) << (i - 64) : 0;
         if (more0) {
           i = first_bit(more0);
-          if ((lead0 >> i) & 1) break;
-          slot = broadcast(s0, i);
+          if ((x.lead0 >> i) & 1) break;
+          slot = broadcast(x.s0, i);
         } else {
-          if (more1 && ((lead1 >> first_bit(more1)) & 1)) break;
+          if (more1 && ((x.lead1 >> first_bit(more1)) & 1)) break;
           covered = false;
-          row = (int64_t)t0 + (more1 ? 64 + first_bit(more1) : 128);
+          row = (int64_t)x.t0 + (more1 ? 64 + first_bit(more1) : 128);
         }
       } else {
-        row += count;
+        row += u.count;
       }
       if (!covered) {
         uint64_t there = 0;
-        int64_t x = -1;
+        int64_t y = -1;
         for (; row < a.rows; row += 64) {
-          x = slot_of(row + lane);
-          there = __ballot(x >= 0);
+          y = slot_of(a, row + lane);
+          there = __ballot(y >= 0);
           if (there) break;
         }
         if (!there) break;
         row += first_bit(there);
-        slot = shuffled(x, first_bit(there));
-        if (slot / kPage != u.page) break;
+        slot = broadcast(y, first_bit(there));
+        if (slot / kPage != page) break;
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // (the next run reads what this one wrote)
+      __syncthreads();           // (the next run reads what this one wrote)
     }
   }
+}
+
+// ------------------------------------------------------ runs of one token
+// The largest of a value over the 16 lanes of a row.
+__device__ __forceinline__ uint32_t row_max_bits(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true));   // (rotations by 8, 4, 2, 1)
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xF, 0xF, true));
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xF, 0xF, true));
+}
+
+template <int IO, int ROPE>
+__device__ __forceinline__ void take_singles(const AppendArgs& a, const Grid& gr, int id, int lane) {
+  id = id * (kWaves) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = gr.singles * (kWaves);
+  const int s = id % waves, rest = id / waves;
+  const int l = rest / gr.windows;
+  const Window x = window_of(a, rest - l * gr.windows, lane);
+  const uint64_t rows = single_rows(x, lane);
+  if (!rows) return;
+  // lane i gets the i-th of these rows
+  const int rank = __popcll(rows & ((1ull << lane) - 1));
+  const bool one = (rows >> lane) & 1;
+  const int order = __builtin_amdgcn_ds_permute((one ? rank : 63) * 4, lane);   // (lane 63 counts only if all are)
+  const int n = __popcll(rows), items = n * a.heads;
+  const int j = lane & 15;
+  for (int first = 4 * s; first < items; first += 4 * waves) {
+    const int item = min(first + (lane >> 4), items - 1);   // (past the end: the last one again, not written)
+    const bool there = first + (lane >> 4) < items;
+    const int r = item / a.heads, h = item - r * a.heads;
+    const int in = n == 64 ? r : __shfl(order, r, 64);
+    const int64_t row = (int64_t)x.t0 + in;
+    const int64_t slot = shuffled(x.s0, in);
+    const int at = (int)(slot % kPage);
+    const int64_t region = ((int64_t)(a.layer0 + l) * a.heads + h) * a.cache.pages + slot / kPage;
+    uint8_t* kp = a.cache.k + region * kPageBytes;
+    uint8_t* vp = a.cache.v + region * kPageBytes;
+    float2* scales = reinterpret_cast<float2*>(a.cache.scales) + region;
+    // lane j of 16: value dimensions 4 j .. 4 j + 3; key dimensions the same, or
+    // 2 j, 2 j + 1 and those 32 further, so that a lane has whole pairs
+    const int64_t ka = l * a.k.layer + row * a.k.row + h * a.k.head, va = l * a.v.layer + row * a.v.row + h * a.v.head;
+    float k[4], v[4];
+    if (ROPE == kHalf) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k[i] = load_element<IO>(a.k.data, ka + 2 * j + (i & 1) + 32 * (i >> 1));
+    } else {
+      load_elements<IO>(a.k.data, ka + 4 * j, k);
+    }
+    load_elements<IO>(a.v.data, va + 4 * j, v);
+    const float2 old = *scales;
+    if (ROPE != kNone) {
+      const float4 c = reinterpret_cast<const float4*>(a.cs)[(int64_t)a.pos[row] * (kDim / 4) + j];
+      if (ROPE == kHalf) {
+        rotate(k[0], k[2], c.x, c.y);
+        rotate(k[1], k[3], c.z, c.w);
+      } else {
+        rotate(k[0], k[1], c.x, c.y);
+        rotate(k[2], k[3], c.z, c.w);
+      }
+    }
+    uint32_t km = 0, vm = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      km = max(km, abs_bits(k[i]));
+      vm = max(vm, abs_bits(v[i]));
+    }
+    km = row_max_bits(km);
+    vm = row_max_bits(vm);
+    const bool bad = max(km, vm) >= kInfBits, fresh = at == 0;
+    const Scale ks = new_scale(bad ? 0 : km, old.x, fresh), vs = new_scale(bad ? 0 : vm, old.y, fresh);
+    // pages whose scale grew: the wave moves one after the other
+    uint64_t moves = __ballot(there && (ks.grown || vs.grown) && j == 0);
+    for (; moves; moves &= moves - 1) {
+      const int i = first_bit(moves);
+      const float by_k = __shfl(ks.move, i, 64), by_v = __shfl(vs.move, i, 64);
+      if (by_k != 1.0f) move_page(reinterpret_cast<uint8_t*>(broadcast((int64_t)kp, i)), by_k, lane);
+      if (by_v != 1.0f) move_page(reinterpret_cast<uint8_t*>(broadcast((int64_t)vp, i)), by_v, lane);
+    }
+    uint32_t kw = codes4(k[0] * ks.inv, k[1] * ks.inv, k[2] * ks.inv, k[3] * ks.inv);
+    uint32_t vw = codes4(v[0] * vs.inv, v[1] * vs.inv, v[2] * vs.inv, v[3] * vs.inv);
+    if (bad) {
+      kw = 0x7F7F7F7Fu;
+      vw = 0;
+    }
+    if (there) {
+      uint8_t* kt = kp + at * kDim;
+      if (ROPE == kHalf) {
+        reinterpret_cast<uint16_t*>(kt)[j] = (uint16_t)kw;
+        reinterpret_cast<uint16_t*>(kt + 32)[j] = (uint16_t)(kw >> 16);
+      } else {
+        reinterpret_cast<uint32_t*>(kt)[j] = kw;
+      }
+      uint8_t* vt = vp + value_byte(at, 4 * j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vt[16 * i] = (uint8_t)(vw >> (8 * i));
+      if (j == 0 && (fresh || ks.grown || vs.grown)) *scales = make_float2(pow2(ks.e), pow2(vs.e));
+    }
+  }
+}
+
+template <int IO, int ROPE>
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Grid gr) {
+  const int lane = threadIdx.x & 63;
+  const int id = blockIdx.x;
+  if (id < gr.blocks_runs)
+    take_runs<IO, ROPE>(a, gr, id, lane);
+  else
+    take_singles<IO, ROPE>(a, gr, id - gr.blocks_runs, lane);
+}
+
+template <int IO>
+hipError_t launch(const AppendArgs& a, const Grid& g, hipStream_t st) {
+  const dim3 grid((unsigned)g.blocks), block(kThreads);
+  if (!a.cs)
+    hipLaunchKernelGGL((append_kernel<IO, kNone>), grid, block, 0, st, a, g);
+  else if (a.rope_half)
+    hipLaunchKernelGGL((append_kernel<IO, kHalf>), grid, block, 0, st, a, g);
+  else
+    hipLaunchKernelGGL((append_kernel<IO, kPairs>), grid, block, 0, st, a, g);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
-  const int windows = (a.rows + 63) / 64;
-  // Waves per window and head: as many as keep the chip's waves busy when
-  // every row is a run of its own, a power of two up to 64.
-  const int64_t base = (int64_t)windows * a.nlayers * a.heads;
-  int share = 1;
-  while (share < 64 && base * share < 8192) share *= 2;
-  const int waves = (int)(base * share);
-  const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
-  if (a.io == kF32)
-    hipLaunchKernelGGL(append_kernel<kF32>, grid, block, 0, st, a, windows, share, waves);
-  else if (a.io == kF16)
-    hipLaunchKernelGGL(append_kernel<kF16>, grid, block, 0, st, a, windows, share, waves);
-  else
-    hipLaunchKernelGGL(append_kernel<kBF16>, grid, block, 0, st, a, windows, share, waves);
-  return hipGetLastError();
+  Grid g;
+  g.windows = (a.rows + 63) / 64;
+  // As many blocks per window as keep the chip busy where every window is full
+  // of runs: at most 32 of several tokens, or 64 of one (sixteen (token, head)s
+  // a block). Fewer where there are many windows: a block that finds nothing costs
+  // its start and the ballots.
+  const int64_t lines = (int64_t)g.windows * a.nlayers;
+  const int64_t most_runs = std::min(32, (a.rows + 1) / 2), most_singles = ((int64_t)std::min(a.rows, 64) * a.heads + 15) / 16;
+  g.share = (int)std::min<int64_t>(most_runs, std::max<int64_t>(2048 / (lines * a.heads), 1));
+  g.singles = (int)std::min<int64_t>(most_singles, std::max<int64_t>(2048 / lines, 1));
+  g.blocks_runs = (int)(lines * a.heads * g.share);
+  g.blocks = (int)(g.blocks_runs + lines * g.singles);
+  if (a.io == kF32) return launch<kF32>(a, g, st);
+  return a.io == kF16 ? launch<kF16>(a, g, st) : launch<kBF16>(a, g, st);
 }
 
 }  // namespace tqp

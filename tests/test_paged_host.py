@@ -126,7 +126,8 @@ def attend(p=_params(), c=_cache(), q=_rows(), rows=5, B=2, layer0=0, nlayers=1,
     (append, dict(layer0=2 ** 31 - 1, nlayers=2 ** 31 - 1), -2, "layers"),
     (append, dict(k=None), -1, "k is"), (append, dict(v=_rows(data=0)), -1, "v is"),
     (append, dict(k=_rows(data=FAKE + 8)), -3, "aligned"), (append, dict(v=_rows(row=516)), -3, "strides"),
-    (append, dict(k=_rows(head=4)), -3, "strides"), (append, dict(slots=0), -1, "NULL"), (append, dict(pos=0), -1, "NULL"),
+    (append, dict(k=_rows(head=4)), -3, "strides"), (append, dict(k=_rows(row=2 ** 23 + 8)), -1, "row strides"),
+    (append, dict(v=_rows(row=-64)), -1, "row strides"), (append, dict(p=_params(rope_positions=2 ** 23 + 1)), -1, "2^23"), (append, dict(slots=0), -1, "NULL"), (append, dict(pos=0), -1, "NULL"),
     (append, dict(p=_params(num_layers=2 ** 20, num_heads=2 ** 20, kv_heads=2 ** 20), nlayers=2 ** 20), -1, "too many"),
     (attend, dict(p=None), -1, "params"), (attend, dict(c=None), -1, "cache"), (attend, dict(q=None), -1, "q is"),
     (attend, dict(rows=-1), -1, "rows"), (attend, dict(B=-1), -1, "B"), (attend, dict(max_len=-1), -1, "max_len"),
