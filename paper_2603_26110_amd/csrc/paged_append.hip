@@ -8,12 +8,11 @@
 // ballots, so that a call needs nothing but slots.
 //
 // The two shapes of a call want different waves, and which one it is only the
-// device knows. So the first part of the grid takes the runs of several tokens
-// (prompts: a block's four waves have a half of the run's keys or values each
-// in their registers), the second the runs of one token (decode steps: four
-// (token, head)s per wave at a time, 16 lanes each); the part that finds nothing
-// in its windows ends after the ballots. (One wave with a whole run took 223
-// registers, so that few waves could wait for memory at once.)
+// device knows. So a block takes its share of the window's runs of several
+// tokens (prompts: the four waves have a half of the run's keys or values each
+// in their registers), then of its runs of one token (decode steps: four per
+// wave at a time, 16 lanes each). (One wave with a whole run took 223 registers,
+// so that few waves could wait for memory at once.)
 //
 // Bound by memory: 256 bytes of fp16 in and 128 out per token and head.
 #include <algorithm>
@@ -26,11 +25,6 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 enum Rope { kNone = 0, kPairs = 1, kHalf = 2 };   // pairs (2m, 2m+1) or (m, m+32)
 constexpr int kFew = 4;          // tokens of a run that is taken token by token
-
-// The grid's two parts: blocks per (window, layer, head) and per (window, layer).
-struct Grid {
-  int windows, share, singles, blocks_runs, blocks;
-};
 
 struct Run {
   int l, h, at, row, count;      // tokens [at, at + count) of the page, from this row on
@@ -50,7 +44,7 @@ __device__ __forceinline__ void rotate(float& a, float& b, float c, float s) {
 // New scale exponent of a page and whether what it holds has to move.
 struct Scale {
   int e;
-  float inv, move;               // 2^-e; 2^(old - e)
+  float by, inv, move;           // 2^e; 2^-e; 2^(old - e)
   bool grown;
 };
 
@@ -60,6 +54,7 @@ __device__ __forceinline__ Scale new_scale(uint32_t amax, float old, bool fresh)
   const int was = exponent_of_scale(old);
   s.grown = !fresh && s.e > was;
   if (!fresh) s.e = max(s.e, was);
+  s.by = pow2(s.e);
   s.inv = pow2(-s.e);
   s.move = s.grown ? pow2(was - s.e) : 1.0f;
   return s;
@@ -91,7 +86,8 @@ __device__ __forceinline__ int value_byte(int t, int d) {
 }
 
 // ------------------------------------------------------- token by token
-// A run of few tokens, or one that holds an infinity or NaN: lane d has
+// A run of few tokens, or one that holds an infinity, NaN or a value that
+// saturates: lane d has
 // dimension d of one token after the other, once for the scales and once for
 // the codes.
 template <int IO, int ROPE>
@@ -135,6 +131,33 @@ __device__ __forceinline__ void append_tokens(const AppendArgs& a, const Run& u,
 }
 
 // ------------------------------------------------------- a run at a time
+// The largest value (its bits) that a scale reaches: 448 * 2^kMaxExp.
+constexpr uint32_t kMostWhole = ((uint32_t)(kMaxExp + 8 + 127) << 23) | 0x600000u;
+
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Values over a scale (a power of two) as codes, without saturation: the same
+// codes as codes4 of the quotients.
+__device__ __forceinline__ uint32_t scaled4(float a, float b, float c, float d, float by) {
+  s16x2 w = {0, 0};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, by, false);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, by, true));
+}
+template <int IO>
+__device__ __forceinline__ uint32_t scaled_pairs(uint32_t ab, uint32_t cd, float by) {
+  s16x2 w = {0, 0};
+  if constexpr (IO == kF16) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(f16x2, ab), by, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(f16x2, cd), by, true);
+  } else {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, ab), by, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, cd), by, true);
+  }
+  return __builtin_bit_cast(uint32_t, w);
+}
+
 // N elements (4 or 2) as they are in memory.
 template <int IO, int N>
 struct Raw {
@@ -171,8 +194,8 @@ __device__ __forceinline__ float element(const Raw<IO, N>& f, int j) {
 // Keys of tokens 32 half .. +31: lane has dimensions [d0, d0+4) and [d1, d1+4)
 // of tokens 32 half + 8 m + lane/8 (the two fours hold whole RoPE pairs). All
 // loads are requested before any is used. top(x) gives the largest of the
-// block's keys, or kInfBits where the run holds what is no number: nothing is
-// written then.
+// block's keys, or kInfBits where the run is to be taken token by token:
+// nothing is written then.
 template <int IO, int ROPE, class Top>
 __device__ __forceinline__ void run_keys(const AppendArgs& a, const Run& u, int half, int lane, Top top) {
   const int end = u.at + u.count, last = end - 1, first = 32 * half + (lane >> 3);
@@ -219,10 +242,10 @@ __device__ __forceinline__ void run_keys(const AppendArgs& a, const Run& u, int 
       }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) km = max(km, abs_bits(k[m][j]));
+    for (int j = 0; j < 8; j += 2) km = max(km, max(abs_bits(k[m][j]), abs_bits(k[m][j + 1])));
   }
   km = top(wave_max_uniform(km));
-  if (km >= kInfBits) return;
+  if (km > kMostWhole) return;
   const Scale s = new_scale(km, old, u.at == 0);
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
@@ -230,8 +253,7 @@ __device__ __forceinline__ void run_keys(const AppendArgs& a, const Run& u, int 
     const bool mine = t >= u.at && t < end;
     uint32_t* p0 = reinterpret_cast<uint32_t*>(u.k + (uint32_t)(t * kDim + d0));
     uint32_t* p1 = reinterpret_cast<uint32_t*>(u.k + (uint32_t)(t * kDim + d1));
-    uint32_t w0 = codes4(k[m][0] * s.inv, k[m][1] * s.inv, k[m][2] * s.inv, k[m][3] * s.inv);
-    uint32_t w1 = codes4(k[m][4] * s.inv, k[m][5] * s.inv, k[m][6] * s.inv, k[m][7] * s.inv);
+    uint32_t w0 = scaled4(k[m][0], k[m][1], k[m][2], k[m][3], s.by), w1 = scaled4(k[m][4], k[m][5], k[m][6], k[m][7], s.by);
     if (s.grown) {               // (uniform)
       const uint32_t o0 = rescale4(*p0, s.move), o1 = rescale4(*p1, s.move);
       w0 = mine ? w0 : o0;
@@ -271,18 +293,36 @@ __device__ __forceinline__ void run_values(const AppendArgs& a, const Run& u, in
     was[1] = vp[1];
   }
   uint32_t vm = 0;
+  if constexpr (IO == kF32) {
 #pragma unroll
-  for (int n = 0; n < 16; ++n) vm = max(vm, max(abs_bits(element(vr[n], 0)), abs_bits(element(vr[n], 1))));
+    for (int n = 0; n < 16; ++n) vm = max(vm, max(vr[n].w[0] & 0x7FFFFFFFu, vr[n].w[1] & 0x7FFFFFFFu));
+  } else {
+    // (the order of the bits is the order of the sizes in these types, too)
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int n = 0; n < 16; ++n) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, vr[n].w[0] & 0x7FFF7FFFu));
+    Raw<IO, 2> most;
+    most.w[0] = max(m[0], m[1]);
+    vm = abs_bits(element(most, 0));
+  }
   vm = top(wave_max_uniform(vm));
-  if (vm >= kInfBits) return;
+  if (vm > kMostWhole) return;
   const Scale s = new_scale(vm, old, u.at == 0);
   u32x4 w[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (IO == kF32) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[j][i] = codes4(element(vr[4 * i], j) * s.inv, element(vr[4 * i + 1], j) * s.inv, element(vr[4 * i + 2], j) * s.inv,
-                       element(vr[4 * i + 3], j) * s.inv);
+      for (int j = 0; j < 2; ++j)
+        w[j][i] = scaled4(element(vr[4 * i], j), element(vr[4 * i + 1], j), element(vr[4 * i + 2], j), element(vr[4 * i + 3], j), s.by);
+    } else {
+      // two dimensions of two tokens to a word, then the dimensions apart
+      const uint32_t a01 = scaled_pairs<IO>(vr[4 * i].w[0], vr[4 * i + 1].w[0], s.by);
+      const uint32_t a23 = scaled_pairs<IO>(vr[4 * i + 2].w[0], vr[4 * i + 3].w[0], s.by);
+      w[0][i] = __builtin_amdgcn_perm(a23, a01, 0x06040200);
+      w[1][i] = __builtin_amdgcn_perm(a23, a01, 0x07050301);
+    }
+  }
   if (u.count < kPage) {
     // the other tokens' bytes stay, or move to the new scale
 #pragma unroll
@@ -373,8 +413,8 @@ __device__ __forceinline__ Window window_of(const AppendArgs& a, int w, int lane
   const int64_t last = broadcast(x.s0, last_bit(x.v0));
   const int64_t n0 = shuffled(x.s0, last_bit((x.v0 & lower) | 1)), n1 = shuffled(x.s1, last_bit((x.v1 & lower) | 1));
   const int64_t before0 = x.v0 & lower ? n0 : carry, before1 = x.v1 & lower ? n1 : last;
-  const bool chained0 = x.s0 >= 0 && before0 >= 0 && x.s0 / kPage == before0 / kPage;
-  const bool chained1 = x.s1 >= 0 && x.s1 / kPage == before1 / kPage;
+  const bool chained0 = x.s0 >= 0 && before0 >= 0 && x.s0 >> 6 == before0 >> 6;
+  const bool chained1 = x.s1 >= 0 && x.s1 >> 6 == before1 >> 6;
   const uint64_t b0 = x.v0 << 1 | (beside ? 1 : 0), b1 = x.v1 << 1 | x.v0 >> 63;
   x.f0 = __ballot(chained0 && ((b0 >> lane) & 1) && x.s0 == before0 + 1);
   x.f1 = __ballot(chained1 && ((b1 >> lane) & 1) && x.s1 == before1 + 1);
@@ -394,21 +434,17 @@ __device__ __forceinline__ uint64_t single_rows(const Window& x, int lane) {
 
 // ------------------------------------------------- runs of several tokens
 template <int IO, int ROPE>
-__device__ __forceinline__ void take_runs(const AppendArgs& a, const Grid& gr, int id, int lane) {
+__device__ __forceinline__ void take_runs(const AppendArgs& a, const Window& x, uint64_t todo, int l, int h, int s, int share,
+                                          int lane) {
   __shared__ uint32_t s_top[2][kWaves];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int turn = 0;
-  const int h = id % a.heads, line = id / a.heads;
-  const int s = line % gr.share, rest = line / gr.share;
-  const int l = rest / gr.windows;
-  const Window x = window_of(a, rest - l * gr.windows, lane);
-  uint64_t todo = x.lead0 & ~single_rows(x, lane);
   for (int n = 0; todo; ++n) {
     int i = first_bit(todo);
     todo &= todo - 1;
-    if (n % gr.share != s) continue;
+    if (n % share != s) continue;
     int64_t row, slot = broadcast(x.s0, i);
-    const int page = (int)(slot / kPage);
+    const int page = (int)(slot >> 6);
     const int64_t region = ((int64_t)(a.layer0 + l) * a.heads + h) * a.cache.pages + page;
     Run u;
     u.l = l;
@@ -424,10 +460,10 @@ __device__ __forceinline__ void take_runs(const AppendArgs& a, const Grid& gr, i
         row = (int64_t)x.t0 + i;
         u.count = min(after == ~0ull ? 64 : first_bit(~after), 63) + 1;
       } else {
-        const uint64_t on = __ballot(slot_of(a, row + lane) == slot + lane && slot % kPage + lane < kPage);
+        const uint64_t on = __ballot(slot_of(a, row + lane) == slot + lane && (slot & 63) + lane < kPage);
         u.count = on == ~0ull ? 64 : first_bit(~on);
       }
-      u.at = (int)(slot % kPage);
+      u.at = (int)(slot & 63);
       u.row = (int)row;
       bool whole = u.count > kFew;
       if (whole) {
@@ -438,7 +474,7 @@ __device__ __forceinline__ void take_runs(const AppendArgs& a, const Grid& gr, i
           if (lane == 0) s_top[turn][wave] = x;
           __syncthreads();
           const uint32_t k = max(s_top[turn][0], s_top[turn][1]), v = max(s_top[turn][2], s_top[turn][3]);
-          whole = max(k, v) < kInfBits;
+          whole = max(k, v) <= kMostWhole;
           return uniform(whole ? (wave < 2 ? k : v) : kInfBits);
         };
         if (wave < 2)
@@ -475,7 +511,7 @@ __device__ __forceinline__ void take_runs(const AppendArgs& a, const Grid& gr, i
         if (!there) break;
         row += first_bit(there);
         slot = broadcast(y, first_bit(there));
-        if (slot / kPage != page) break;
+        if ((slot >> 6) != page) break;
       }
       __syncthreads();           // (the next run reads what this one wrote)
     }
@@ -492,29 +528,21 @@ __device__ __forceinline__ uint32_t row_max_bits(uint32_t v) {
 }
 
 template <int IO, int ROPE>
-__device__ __forceinline__ void take_singles(const AppendArgs& a, const Grid& gr, int id, int lane) {
-  id = id * (kWaves) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = gr.singles * (kWaves);
-  const int s = id % waves, rest = id / waves;
-  const int l = rest / gr.windows;
-  const Window x = window_of(a, rest - l * gr.windows, lane);
-  const uint64_t rows = single_rows(x, lane);
-  if (!rows) return;
+__device__ __forceinline__ void take_singles(const AppendArgs& a, const Window& x, uint64_t rows, int l, int h, int s, int share,
+                                             int lane) {
   // lane i gets the i-th of these rows
   const int rank = __popcll(rows & ((1ull << lane) - 1));
   const bool one = (rows >> lane) & 1;
   const int order = __builtin_amdgcn_ds_permute((one ? rank : 63) * 4, lane);   // (lane 63 counts only if all are)
-  const int n = __popcll(rows), items = n * a.heads;
-  const int j = lane & 15;
-  for (int first = 4 * s; first < items; first += 4 * waves) {
-    const int item = min(first + (lane >> 4), items - 1);   // (past the end: the last one again, not written)
-    const bool there = first + (lane >> 4) < items;
-    const int r = item / a.heads, h = item - r * a.heads;
-    const int in = n == 64 ? r : __shfl(order, r, 64);
+  const int n = __popcll(rows), j = lane & 15;
+  for (int first = 16 * s + 4 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); first < n; first += 16 * share) {
+    const int item = min(first + (lane >> 4), n - 1);   // (past the end: the last one again, not written)
+    const bool there = first + (lane >> 4) < n;
+    const int in = n == 64 ? item : __shfl(order, item, 64);
     const int64_t row = (int64_t)x.t0 + in;
     const int64_t slot = shuffled(x.s0, in);
-    const int at = (int)(slot % kPage);
-    const int64_t region = ((int64_t)(a.layer0 + l) * a.heads + h) * a.cache.pages + slot / kPage;
+    const int at = (int)(slot & 63);
+    const int64_t region = ((int64_t)(a.layer0 + l) * a.heads + h) * a.cache.pages + (slot >> 6);
     uint8_t* kp = a.cache.k + region * kPageBytes;
     uint8_t* vp = a.cache.v + region * kPageBytes;
     float2* scales = reinterpret_cast<float2*>(a.cache.scales) + region;
@@ -581,44 +609,40 @@ __device__ __forceinline__ void take_singles(const AppendArgs& a, const Grid& gr
 }
 
 template <int IO, int ROPE>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Grid gr) {
-  const int lane = threadIdx.x & 63;
-  const int id = blockIdx.x;
-  if (id < gr.blocks_runs)
-    take_runs<IO, ROPE>(a, gr, id, lane);
-  else
-    take_singles<IO, ROPE>(a, gr, id - gr.blocks_runs, lane);
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int windows, int share) {
+  const int lane = threadIdx.x & 63, id = blockIdx.x;
+  const int h = id % a.heads, line = id / a.heads;
+  const int s = line % share, rest = line / share;
+  const int l = rest / windows;
+  const Window x = window_of(a, rest - l * windows, lane);
+  if (!x.lead0) return;
+  const uint64_t singles = single_rows(x, lane), runs = x.lead0 & ~singles;
+  if (runs) take_runs<IO, ROPE>(a, x, runs, l, h, s, share, lane);
+  if (singles) take_singles<IO, ROPE>(a, x, singles, l, h, s, share, lane);
 }
 
 template <int IO>
-hipError_t launch(const AppendArgs& a, const Grid& g, hipStream_t st) {
-  const dim3 grid((unsigned)g.blocks), block(kThreads);
+hipError_t launch(const AppendArgs& a, hipStream_t st) {
+  const int windows = (a.rows + 63) / 64;
+  // Sixteen rows a block where every row is a run of its own and that fills the
+  // chip; the whole window where there are windows enough.
+  const int64_t lines = (int64_t)windows * a.nlayers * a.heads;
+  const int share = (int)std::min<int64_t>((std::min(a.rows, 64) + 15) / 16, std::max<int64_t>(4096 / lines, 1));
+  const dim3 grid((unsigned)(lines * share)), block(kThreads);
   if (!a.cs)
-    hipLaunchKernelGGL((append_kernel<IO, kNone>), grid, block, 0, st, a, g);
+    hipLaunchKernelGGL((append_kernel<IO, kNone>), grid, block, 0, st, a, windows, share);
   else if (a.rope_half)
-    hipLaunchKernelGGL((append_kernel<IO, kHalf>), grid, block, 0, st, a, g);
+    hipLaunchKernelGGL((append_kernel<IO, kHalf>), grid, block, 0, st, a, windows, share);
   else
-    hipLaunchKernelGGL((append_kernel<IO, kPairs>), grid, block, 0, st, a, g);
+    hipLaunchKernelGGL((append_kernel<IO, kPairs>), grid, block, 0, st, a, windows, share);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
-  Grid g;
-  g.windows = (a.rows + 63) / 64;
-  // As many blocks per window as keep the chip busy where every window is full
-  // of runs: at most 32 of several tokens, or 64 of one (sixteen (token, head)s
-  // a block). Fewer where there are many windows: a block that finds nothing costs
-  // its start and the ballots.
-  const int64_t lines = (int64_t)g.windows * a.nlayers;
-  const int64_t most_runs = std::min(32, (a.rows + 1) / 2), most_singles = ((int64_t)std::min(a.rows, 64) * a.heads + 15) / 16;
-  g.share = (int)std::min<int64_t>(most_runs, std::max<int64_t>(2048 / (lines * a.heads), 1));
-  g.singles = (int)std::min<int64_t>(most_singles, std::max<int64_t>(2048 / lines, 1));
-  g.blocks_runs = (int)(lines * a.heads * g.share);
-  g.blocks = (int)(g.blocks_runs + lines * g.singles);
-  if (a.io == kF32) return launch<kF32>(a, g, st);
-  return a.io == kF16 ? launch<kF16>(a, g, st) : launch<kBF16>(a, g, st);
+  if (a.io == kF32) return launch<kF32>(a, st);
+  return a.io == kF16 ? launch<kF16>(a, st) : launch<kBF16>(a, st);
 }
 
 }  // namespace tqp

@@ -186,7 +186,7 @@ __device__ __forceinline__ uint32_t below(int first, int len) {
 
 // ------------------------------------------------------------- few rows
 template <int IO, int PREC, int W>
-__global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, int per_xcd, int tiles) {
+__global__ __launch_bounds__(W * 64, PREC < 2 ? 4 : W == 16 ? 4 : 3) void attend_few(AttendArgs a, int total, int per_xcd, int tiles) {
   constexpr int kStride = kDim + 4;
   __shared__ float s_m[W][kRowsFew], s_l[W][kRowsFew];
   __shared__ __align__(16) float s_o[W * kRowsFew * kStride];
@@ -199,6 +199,10 @@ __global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, in
   const int h = rest % a.kv_heads, b = (rest / a.kv_heads) % a.B, l = rest / a.kv_heads / a.B;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, g = lane >> 4, c16 = lane & 15;
   const Sequence s = sequence_of(a, b);
+  // The table's entries of the pages that the wave starts with, where that does
+  // not depend on the rows' positions: asked for with the sequence's length.
+  const int32_t* table = a.table + (int64_t)b * a.width;
+  int entries = a.nsplit == 1 ? table[min(wave + lane * W, a.width - 1)] : 0;
   if (!s.there) return;
   if (!s.fine) {
     if (tile == 0 && split == 0) refuse<IO>(a, s, l, h);
@@ -239,43 +243,43 @@ __global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, in
   }
 
   const int64_t region = ((int64_t)(a.layer0 + l) * a.kv_heads + h) * a.cache.pages;
-  const uint8_t* kplane = a.cache.k + region * kPageBytes + lane * 16;
-  const uint8_t* vplane = a.cache.v + region * kPageBytes + lane * 16;
+  const uint8_t* kplane = a.cache.k + region * kPageBytes;
+  const uint8_t* vplane = a.cache.v + region * kPageBytes;
+  const uint32_t koff = c16 * kDim + g * 16, voff = g * 1024 + c16 * 16;
   const float2* scales = reinterpret_cast<const float2*>(a.cache.scales) + region;
-  const int32_t* table = a.table + (int64_t)b * a.width;
 
   float m = lowest(), lsum = 0.0f, vscale = 1.0f;
   f32x4 O[4] = {};
 
-  struct Raw {
-    u32x4 k[4], v[4];
-    float2 sc;
+  // One page: its keys (row c16 of the 16 tokens of part j, bytes 16 g .. +15)
+  // and values (dimension 16 j + c16, the sixteen tokens of group g).
+  u32x4 kw[4], vw[4];
+  float2 sc;
+  auto page_of = [&](int i, bool& bad) {
+    const int page = __builtin_amdgcn_readlane(entries, i);
+    bad = page < 0 || page >= a.cache.pages;
+    return bad ? 0 : page;
   };
-  int entries = 0;               // lane i: the table's entry of the wave's i-th page of 64
-  auto load = [&](Raw& w, int i) {
-    int page = __builtin_amdgcn_readlane(entries, i);
-    const bool bad = page < 0 || page >= a.cache.pages;
-    page = bad ? 0 : page;
-    const int64_t at = (int64_t)page * kPageBytes;
-    // keys: row c16 of the 16 tokens of part i, its bytes 16 g .. 16 g + 15
-    const uint8_t* kp = kplane - lane * 16 + at + c16 * kDim + g * 16;
-    // values: dimension 16 i + c16, the sixteen tokens of group g
-    const uint8_t* vp = vplane - lane * 16 + at + g * 1024 + c16 * 16;
+  auto load_keys = [&](int page, bool bad) {
+    const uint8_t* p = kplane + (int64_t)page * kPageBytes;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w.k[j] = *reinterpret_cast<const u32x4*>(kp + j * 1024);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w.v[j] = *reinterpret_cast<const u32x4*>(vp + j * 256);
-    w.sc = scales[page];
+    for (int j = 0; j < 4; ++j) kw[j] = *reinterpret_cast<const u32x4*>(p + koff + j * 1024);
+    sc = scales[page];
     if (bad) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w.k[j] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+      for (int j = 0; j < 4; ++j) kw[j] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
     }
   };
-  auto attend = [&](Raw& w, int tl) {
+  auto load_values = [&](int page) {
+    const uint8_t* p = vplane + (int64_t)page * kPageBytes;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vw[j] = *reinterpret_cast<const u32x4*>(p + voff + j * 256);
+  };
+  auto attend = [&](int tl, int next, bool next_bad) {   // next: the page after this one, or -1
     f32x4 S[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const f16x8 k0 = halves8(w.k[i][0], w.k[i][1]), k1 = halves8(w.k[i][2], w.k[i][3]);
+      const f16x8 k0 = halves8(kw[i][0], kw[i][1]), k1 = halves8(kw[i][2], kw[i][3]);
       f32x4 z = {};
       if (PREC > 0) {
         z = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, ql[0], z, 0, 0, 0);
@@ -284,7 +288,9 @@ __global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, in
       z = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qh[0], z, 0, 0, 0);
       S[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qh[1], z, 0, 0, 0);
     }
-    const float c = score_scale(rowscale, w.sc.x);
+    const float c = score_scale(rowscale, sc.x), vs = sc.y;
+    // (the registers that this page's keys leave take the next one's)
+    if (next >= 0) load_keys(next, next_bad);
     const int tok0 = tl * kPage + 4 * g;
 #pragma unroll
     for (int i = 0; i < 4; ++i) S[i] *= c;
@@ -298,7 +304,7 @@ __global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, in
       for (int i = 0; i < 4; ++i) {
         const uint32_t keep = below(tok0 + 16 * i, s.len);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w.v[j][i] &= keep;
+        for (int j = 0; j < 4; ++j) vw[j][i] &= keep;
       }
     }
     float top = S[0][0];
@@ -315,9 +321,9 @@ __global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, in
 #pragma unroll
       for (int i = 0; i < 4; ++i) O[i] *= f;
     }
-    if (w.sc.y != vscale) {      // (uniform: O is in units of the page's value scale)
-      const float f = vscale / w.sc.y;
-      vscale = w.sc.y;
+    if (vs != vscale) {      // (uniform: O is in units of the page's value scale)
+      const float f = vscale / vs;
+      vscale = vs;
 #pragma unroll
       for (int i = 0; i < 4; ++i) O[i] *= f;
     }
@@ -333,7 +339,7 @@ __global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, in
       }
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
-      const f16x8 v0 = halves8(w.v[d][0], w.v[d][1]), v1 = halves8(w.v[d][2], w.v[d][3]);
+      const f16x8 v0 = halves8(vw[d][0], vw[d][1]), v1 = halves8(vw[d][2], vw[d][3]);
       if (PREC > 1) {
         O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pl[0], O[d], 0, 0, 0);
         O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pl[1], O[d], 0, 0, 0);
@@ -341,16 +347,18 @@ __global__ __launch_bounds__(W * 64) void attend_few(AttendArgs a, int total, in
       O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, ph[0], O[d], 0, 0, 0);
       O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, ph[1], O[d], 0, 0, 0);
     }
+    if (next >= 0) load_values(next);
   };
   for (int first = begin; first < end; first += 64 * W) {
     const int n = min(64, (end - first + W - 1) / W);
-    entries = lane < n ? table[first + lane * W] : 0;
-    Raw cur, next;
-    load(cur, 0);
+    if (a.nsplit > 1 || first > begin) entries = lane < n ? table[first + lane * W] : 0;
+    bool bad;
+    int page = page_of(0, bad);
+    load_keys(page, bad);
+    load_values(page);
     for (int i = 0; i < n; ++i) {
-      if (i + 1 < n) load(next, i + 1);
-      attend(cur, first + i * W);
-      cur = next;
+      page = i + 1 < n ? page_of(i + 1, bad) : -1;
+      attend(first + i * W, page, bad);
     }
   }
   lsum += __shfl_xor(lsum, 16, 64);
