@@ -23,7 +23,6 @@ namespace tqp {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-enum Rope { kNone = 0, kPairs = 1, kHalf = 2 };   // pairs (2m, 2m+1) or (m, m+32)
 constexpr int kFew = 4;          // tokens of a run that is taken token by token
 
 struct Run {

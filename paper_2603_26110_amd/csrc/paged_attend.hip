@@ -122,30 +122,78 @@ __device__ __forceinline__ Row row_of(const AttendArgs& a, const Sequence& s, in
   return r;
 }
 
-// Dimensions d0 .. d0+N-1 of a row, rotated (their partners are among them, or
-// 32 away in the half pairing).
+// Dimensions d0 .. d0+N-1 of a query row with what rotates them (their partners
+// are among them, or 32 away in the half pairing), as loaded; and rotated. Apart
+// so that other loads can be asked for between. (A row that is not fine takes
+// position 0: its result is not used.)
+template <int IO, int N, int ROPE>
+struct Query {
+  static constexpr int kWords = IO == kF32 ? N : N / 2;
+  uint32_t x[kWords], o[ROPE == kHalf ? kWords : 1];
+  float2 c[ROPE == kHalf ? N : ROPE == kPairs ? N / 2 : 1];
+};
+
 template <int IO, int N>
-__device__ __forceinline__ void load_query(const AttendArgs& a, const Row& r, int l, int d0, float (&x)[N]) {
+__device__ __forceinline__ void load_words(const void* base, int64_t at, uint32_t* w) {
+  const u32x4* p = reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(base) + at * io_bytes<IO>());
+#pragma unroll
+  for (int i = 0; i < (IO == kF32 ? N : N / 2) / 4; ++i) {
+    const u32x4 v = p[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+  }
+}
+
+template <int IO, int N, int ROPE>
+__device__ __forceinline__ void load_query(const AttendArgs& a, const Row& r, int l, int d0, Query<IO, N, ROPE>& q) {
   const int64_t at = l * a.q.layer + r.row * a.q.row + r.head * a.q.head;
-  load_elements<IO>(a.q.data, at + d0, x);
-  if (!a.cs || !r.fine) return;
-  const float2* cs = reinterpret_cast<const float2*>(a.cs) + (int64_t)r.pos * (kDim / 2);
-  if (a.rope_half) {
-    float o[N];
-    load_elements<IO>(a.q.data, at + (d0 ^ 32), o);
+  load_words<IO, N>(a.q.data, at + d0, q.x);
+  if constexpr (ROPE == kNone) return;
+  const float4* cs = reinterpret_cast<const float4*>(a.cs) + (int64_t)(r.fine ? r.pos : 0) * (kDim / 4);
+  if constexpr (ROPE == kHalf) {
+    load_words<IO, N>(a.q.data, at + (d0 ^ 32), q.o);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float4 c = cs[((d0 & 31) + i) >> 1];
+      q.c[i] = make_float2(c.x, c.y);
+      q.c[i + 1] = make_float2(c.z, c.w);
+    }
+  } else if constexpr (ROPE == kPairs) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 c = cs[(d0 + i) >> 2];
+      q.c[i / 2] = make_float2(c.x, c.y);
+      q.c[i / 2 + 1] = make_float2(c.z, c.w);
+    }
+  }
+}
+
+template <int IO>
+__device__ __forceinline__ float entry(const uint32_t* w, int i) {
+  if constexpr (IO == kF32) return __uint_as_float(w[i]);
+  const uint32_t bits = (w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu;
+  if constexpr (IO == kBF16) return __uint_as_float(bits << 16);
+  return __half2float(__ushort_as_half((unsigned short)bits));
+}
+
+template <int IO, int N, int ROPE>
+__device__ __forceinline__ void rotate_query(const Query<IO, N, ROPE>& q, int d0, float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = entry<IO>(q.x, i);
+  if constexpr (ROPE == kHalf) {
     const bool second = (d0 & 32) != 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float2 c = cs[(d0 & 31) + i];
-      x[i] = second ? o[i] * c.y + x[i] * c.x : x[i] * c.x - o[i] * c.y;
+      const float o = entry<IO>(q.o, i);
+      x[i] = second ? o * q.c[i].y + x[i] * q.c[i].x : x[i] * q.c[i].x - o * q.c[i].y;
     }
-  } else {
+  } else if constexpr (ROPE == kPairs) {
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
-      const float2 c = cs[(d0 + i) >> 1];
-      const float p = x[i] * c.x - x[i + 1] * c.y, q = x[i] * c.y + x[i + 1] * c.x;
-      x[i] = p;
-      x[i + 1] = q;
+      const float2 c = q.c[i / 2];
+      const float u = x[i] * c.x - x[i + 1] * c.y, v = x[i] * c.y + x[i + 1] * c.x;
+      x[i] = u;
+      x[i + 1] = v;
     }
   }
 }
@@ -185,8 +233,8 @@ __device__ __forceinline__ uint32_t below(int first, int len) {
 }
 
 // ------------------------------------------------------------- few rows
-template <int IO, int PREC, int W>
-__global__ __launch_bounds__(W * 64, PREC < 2 ? 4 : W == 16 ? 4 : 3) void attend_few(AttendArgs a, int total, int per_xcd, int tiles) {
+template <int IO, int PREC, int ROPE, int W>
+__global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendArgs a, int total, int per_xcd, int tiles) {
   constexpr int kStride = kDim + 4;
   __shared__ float s_m[W][kRowsFew], s_l[W][kRowsFew];
   __shared__ __align__(16) float s_o[W * kRowsFew * kStride];
@@ -225,23 +273,8 @@ __global__ __launch_bounds__(W * 64, PREC < 2 ? 4 : W == 16 ? 4 : 3) void attend
   if (split >= parts) return;
   const int begin = split * st + wave, end = min(ntiles, (split + 1) * st);
 
-  // q': lane (g, column) has dimensions 16 g .. 16 g + 15 of its row
-  f16x8 qh[2], ql[2];
-  float rowscale;
-  {
-    float x[16];
-    load_query<IO>(a, r, l, 16 * g, x);
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) m = max(m, abs_bits(x[i]));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
-    const int e = row_exponent(m);
-    split8<PREC>(x, e, qh[0], ql[0]);
-    split8<PREC>(x + 8, e, qh[1], ql[1]);
-    rowscale = a.scale2 * pow2(max(e, -126));
-  }
-
+  Query<IO, 16, ROPE> query;
+  load_query(a, r, l, 16 * g, query);
   const int64_t region = ((int64_t)(a.layer0 + l) * a.kv_heads + h) * a.cache.pages;
   const uint8_t* kplane = a.cache.k + region * kPageBytes;
   const uint8_t* vplane = a.cache.v + region * kPageBytes;
@@ -275,6 +308,34 @@ __global__ __launch_bounds__(W * 64, PREC < 2 ? 4 : W == 16 ? 4 : 3) void attend
 #pragma unroll
     for (int j = 0; j < 4; ++j) vw[j] = *reinterpret_cast<const u32x4*>(p + voff + j * 256);
   };
+  // The wave's first keys, before the query is worked on (with the values, too,
+  // registers would spill).
+  auto start = [&](int first) {
+    if (a.nsplit > 1 || first > begin) entries = lane < (end - first + W - 1) / W ? table[first + lane * W] : 0;
+    bool bad;
+    const int page = page_of(0, bad);
+    load_keys(page, bad);
+    return page;
+  };
+  int page = begin < end ? start(begin) : 0;
+
+  // q': lane (g, column) has dimensions 16 g .. 16 g + 15 of its row
+  f16x8 qh[2], ql[2];
+  float rowscale;
+  {
+    float x[16];
+    rotate_query(query, 16 * g, x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, abs_bits(x[i]));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+    const int e = row_exponent(m);
+    split8<PREC>(x, e, qh[0], ql[0]);
+    split8<PREC>(x + 8, e, qh[1], ql[1]);
+    rowscale = a.scale2 * pow2(max(e, -126));
+  }
+
   auto attend = [&](int tl, int next, bool next_bad) {   // next: the page after this one, or -1
     f32x4 S[4];
 #pragma unroll
@@ -351,12 +412,10 @@ __global__ __launch_bounds__(W * 64, PREC < 2 ? 4 : W == 16 ? 4 : 3) void attend
   };
   for (int first = begin; first < end; first += 64 * W) {
     const int n = min(64, (end - first + W - 1) / W);
-    if (a.nsplit > 1 || first > begin) entries = lane < n ? table[first + lane * W] : 0;
-    bool bad;
-    int page = page_of(0, bad);
-    load_keys(page, bad);
+    if (first > begin) page = start(first);
     load_values(page);
     for (int i = 0; i < n; ++i) {
+      bool bad = false;
       page = i + 1 < n ? page_of(i + 1, bad) : -1;
       attend(first + i * W, page, bad);
     }
@@ -442,7 +501,7 @@ __global__ __launch_bounds__(W * 64, PREC < 2 ? 4 : W == 16 ? 4 : 3) void attend
 }
 
 // ------------------------------------------------------------ many rows
-template <int IO, int PREC>
+template <int IO, int PREC, int ROPE>
 __global__ __launch_bounds__(256) void attend_many(AttendArgs a, int total, int per_xcd, int tiles) {
   const int work = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
   if (work >= total) return;
@@ -474,7 +533,9 @@ __global__ __launch_bounds__(256) void attend_many(AttendArgs a, int total, int 
   float rowscale;
   {
     float x[32];
-    load_query<IO>(a, r, l, 32 * half, x);
+    Query<IO, 32, ROPE> query;
+    load_query(a, r, l, 32 * half, query);
+    rotate_query(query, 32 * half, x);
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 32; ++i) m = max(m, abs_bits(x[i]));
@@ -617,24 +678,41 @@ AttendPlan plan_attend(int64_t units0, int64_t rows, int max_len) {
   p.waves = 4;
   if (!p.few) return p;
   const int64_t pages = std::max<int64_t>((max_len + (int64_t)kPage - 1) / kPage, 1);
-  // Blocks of four waves, about four per compute unit, every wave with a page.
-  const int64_t want = std::max<int64_t>(1024 / std::max<int64_t>(p.units, 1), 1);
-  p.nsplit = (int)std::min<int64_t>(std::min<int64_t>(want, (pages + p.waves - 1) / p.waves), kMaxSplit);
+  // Eight waves a block where the units leave compute units free and there are
+  // pages for them (20 units of 17 pages 8.8 -> 8.2 us, 160 of 33 17.9 -> 14.4),
+  // or where there are so many pages that joining the waves costs nothing (640
+  // units of 128 pages 128 -> 126 us); four else (660 units of 17 pages 22.7
+  // against 27.3 us: more blocks fit a compute unit at once).
+  if ((p.units <= 256 && pages >= 16) || pages >= 64) p.waves = 8;
+  // A unit's pages are shared by blocks, with two pages a wave, where the blocks
+  // find free compute units and each wave is spared two and a half pages, at
+  // about 1.1 us each: storing and joining costs 2.5 us and more (20 units of
+  // 128 pages 23.8 -> 12.4 us; 64 units of 17 pages would go 9.4 -> 10.7).
+  const int64_t split = std::min<int64_t>(std::min<int64_t>(256 / p.units, pages / 16), kMaxSplit);
+  if (p.waves == 8 && split > 1 && pages * (split - 1) >= 20 * split) p.nsplit = (int)split;
   if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * kPart * sizeof(float);
   return p;
 }
 
 namespace {
 
-template <int IO, int PREC>
+template <int IO, int PREC, int ROPE>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   const int64_t total = p.units * p.nsplit, per_xcd = (total + kXcds - 1) / kXcds;
-  const dim3 grid((unsigned)(per_xcd * kXcds));
-  if (p.few)
-    hipLaunchKernelGGL((attend_few<IO, PREC, 4>), grid, dim3(256), 0, st, a, (int)total, (int)per_xcd, p.tiles);
+  const dim3 grid((unsigned)(per_xcd * kXcds)), block(p.waves * 64);
+  if (!p.few)
+    hipLaunchKernelGGL((attend_many<IO, PREC, ROPE>), grid, block, 0, st, a, (int)total, (int)per_xcd, p.tiles);
+  else if (p.waves == 8)
+    hipLaunchKernelGGL((attend_few<IO, PREC, ROPE, 8>), grid, block, 0, st, a, (int)total, (int)per_xcd, p.tiles);
   else
-    hipLaunchKernelGGL((attend_many<IO, PREC>), grid, dim3(256), 0, st, a, (int)total, (int)per_xcd, p.tiles);
+    hipLaunchKernelGGL((attend_few<IO, PREC, ROPE, 4>), grid, block, 0, st, a, (int)total, (int)per_xcd, p.tiles);
   return hipGetLastError();
+}
+
+template <int IO, int PREC>
+hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  if (!a.cs) return launch<IO, PREC, kNone>(a, p, st);
+  return a.rope_half ? launch<IO, PREC, kHalf>(a, p, st) : launch<IO, PREC, kPairs>(a, p, st);
 }
 
 }  // namespace

@@ -16,6 +16,7 @@ constexpr int kMinExp = -48, kMaxExp = 47;   // of a page's scale
 constexpr float kCodeMax = 448.0f;           // largest e4m3 value
 
 enum Io { kF32 = 0, kF16 = 1, kBF16 = 2 };
+enum Rope { kNone = 0, kPairs = 1, kHalf = 2 };   // pairs (2m, 2m+1) or (m, m+32)
 
 struct Rows {
   const void* data;
