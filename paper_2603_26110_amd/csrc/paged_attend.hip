@@ -49,6 +49,13 @@ __device__ __forceinline__ f16x8 halves8(uint32_t lo, uint32_t hi) {
   return __builtin_bit_cast(f16x8, w);
 }
 
+__device__ __forceinline__ f16x2 half2_of(_Float16 a, _Float16 b) { return f16x2{a, b}; }
+
+// The larger of two numbers, NaN if one is none (an instruction takes three; the
+// maximum that ignores a NaN costs one more for each operand). A row with a NaN
+// score has a NaN result, whatever its maximum.
+__device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 __device__ __forceinline__ float max_across32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
   return fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
@@ -501,22 +508,36 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
 }
 
 // ------------------------------------------------------------ many rows
+// Four waves of 32 rows share a page: each thread loads 16 bytes of its keys and
+// values, converts them to fp16 and leaves them in LDS as the matrix
+// instructions take them (16 bytes a lane, read without conflicts). While one
+// page is worked on the next one's codes are on their way in registers, and one
+// barrier a page is enough for two buffers. Conversions and loads so cost a
+// quarter of what they would with a page per wave; what remains is bound by the
+// vector unit: per score one exponential (quarter rate), a multiply-add, half a
+// maximum, half a conversion and half a sum.
+constexpr int kFrag = 64 * 16;                        // bytes of an operand of one instruction
+
 template <int IO, int PREC, int ROPE>
-__global__ __launch_bounds__(256) void attend_many(AttendArgs a, int total, int per_xcd, int tiles) {
+__global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, int per_xcd, int tiles) {
+  // [buffer][keys: 32-token half T, step | values: 32-dimension half, step][lane]
+  __shared__ __align__(16) uint8_t s_page[2][16 * kFrag];
+  __shared__ int s_most[4];
   const int work = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
   if (work >= total) return;
   // (the last rows first: under a causal mask they see the most)
   const int tile = tiles - 1 - work % tiles, rest = work / tiles;
   const int h = rest % a.kv_heads, b = (rest / a.kv_heads) % a.B, l = rest / a.kv_heads / a.B;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, c32 = lane & 31;
+  const int lane = threadIdx.x & 63, half = lane >> 5, c32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Sequence s = sequence_of(a, b);
   if (!s.there) return;
   if (!s.fine) {
     if (tile == 0) refuse<IO>(a, s, l, h);
     return;
   }
+  if (tile * 4 * kRowsMany >= s.n * a.group) return;
   const int f0 = (tile * 4 + wave) * kRowsMany;
-  if (f0 >= s.n * a.group) return;
   const Row r = row_of(a, s, h, f0 + c32);
   int most = r.sees, least = r.fine ? r.sees : INT_MAX;
 #pragma unroll
@@ -526,7 +547,58 @@ __global__ __launch_bounds__(256) void attend_many(AttendArgs a, int total, int 
   }
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
-  const int ntiles = (most + kPage - 1) / kPage;
+  if (lane == 0) s_most[wave] = most;
+  __syncthreads();
+  const int mine = (most + kPage - 1) / kPage;        // pages that the wave's rows see, and the block's
+  const int ntiles = (__builtin_amdgcn_readfirstlane(max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]))) + kPage - 1) / kPage;
+
+  const int64_t region = ((int64_t)(a.layer0 + l) * a.kv_heads + h) * a.cache.pages;
+  const uint8_t* kplane = a.cache.k + region * kPageBytes;
+  const uint8_t* vplane = a.cache.v + region * kPageBytes;
+  const float2* scales = reinterpret_cast<const float2*>(a.cache.scales) + region;
+  const int32_t* table = a.table + (int64_t)b * a.width;
+
+  // A thread's part of a page: 16 dimensions of a token's key (token
+  // threadIdx/4, dimensions 16 (threadIdx%4) ..), 16 tokens of a dimension's
+  // value (group `wave`, dimension `lane`).
+  u32x4 kw, vw;
+  float2 sc = make_float2(1.0f, 1.0f);
+  auto load = [&](int page) {
+    const bool bad = page < 0 || page >= a.cache.pages;
+    page = bad ? 0 : page;
+    kw = *reinterpret_cast<const u32x4*>(kplane + (int64_t)page * kPageBytes + threadIdx.x * 16);
+    vw = *reinterpret_cast<const u32x4*>(vplane + (int64_t)page * kPageBytes + threadIdx.x * 16);
+    sc = scales[page];
+    if (bad) kw = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+  };
+  // Key operands: step i, lane (half, token): dimensions 32 half + 8 i .. +7.
+  // (the token's place within an operand is turned by what the four threads of
+  // a token differ in, so that their stores go to different banks)
+  const int tok = threadIdx.x >> 2, cc = threadIdx.x & 3;
+  const uint32_t kto = ((tok >> 5) * 4 + 2 * (cc & 1)) * kFrag + ((cc >> 1) * 32 + ((tok & 31) ^ (4 * (cc & 1) + 8 * (cc >> 1)))) * 16;
+  // Value operands: step u, lane (half, dimension): tokens 16 u + 4 half + r and
+  // 16 u + 8 + 4 half + r.
+  const uint32_t vto = (8 + (lane >> 5) * 4) * kFrag + ((wave & 1) * 32 + c32) * 16 + (wave >> 1) * 8;
+  auto stage = [&](uint8_t* to, int tl) {
+    *reinterpret_cast<f16x8*>(to + kto) = halves8(kw[0], kw[1]);
+    *reinterpret_cast<f16x8*>(to + kto + kFrag) = halves8(kw[2], kw[3]);
+    if ((tl + 1) * kPage > s.len) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vw[i] &= below(tl * kPage + 16 * i + 4 * wave, s.len);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      const f16x8 v = halves8(vw[i], vw[i + 1]);
+      const u32x4 w = __builtin_bit_cast(u32x4, v);
+      *reinterpret_cast<u32x2*>(to + vto + i * kFrag) = u32x2{w[0], w[1]};
+      *reinterpret_cast<u32x2*>(to + vto + (i + 1) * kFrag) = u32x2{w[2], w[3]};
+    }
+  };
+  int page = 0;                  // table entry of the page to load next
+  if (ntiles > 0) {
+    load(table[0]);
+    page = table[min(1, ntiles - 1)];
+  }
 
   // q': lane (half, column) has dimensions 32 half .. +31 of its row
   f16x8 qh[4], ql[4];
@@ -545,114 +617,92 @@ __global__ __launch_bounds__(256) void attend_many(AttendArgs a, int total, int 
     for (int i = 0; i < 4; ++i) split8<PREC>(x + 8 * i, e, qh[i], ql[i]);
     rowscale = a.scale2 * pow2(max(e, -126));
   }
-  const int64_t region = ((int64_t)(a.layer0 + l) * a.kv_heads + h) * a.cache.pages;
-  const uint8_t* kplane = a.cache.k + region * kPageBytes + c32 * kDim + half * 32;
-  const uint8_t* vplane = a.cache.v + region * kPageBytes + half * 1024 + c32 * 16;
-  const float2* scales = reinterpret_cast<const float2*>(a.cache.scales) + region;
-  const int32_t* table = a.table + (int64_t)b * a.width;
 
   float m = lowest(), lsum = 0.0f, vscale = 1.0f;
   f32x16 O[2] = {};
-  struct Raw {
-    u32x4 k[2][2], v[2][2];      // [tokens 32 T ..][half of the row's part]; [dimensions 32 t ..][groups half, half + 2]
-    float2 sc;
-  };
-  auto load = [&](Raw& w, int tl) {
-    int page = table[tl];
-    const bool bad = page < 0 || page >= a.cache.pages;
-    page = bad ? 0 : page;
-    const uint8_t* kp = kplane + (int64_t)page * kPageBytes;
-    const uint8_t* vp = vplane + (int64_t)page * kPageBytes;
-#pragma unroll
-    for (int T = 0; T < 2; ++T)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        w.k[T][j] = *reinterpret_cast<const u32x4*>(kp + T * 2048 + j * 16);
-        w.v[T][j] = *reinterpret_cast<const u32x4*>(vp + T * 512 + j * 2048);
-      }
-    w.sc = scales[page];
-    if (bad) {
-#pragma unroll
-      for (int T = 0; T < 2; ++T)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) w.k[T][j] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+  const uint32_t kfrom[2] = {(uint32_t)(32 * half + (c32 ^ (8 * half))) * 16, (uint32_t)(32 * half + (c32 ^ (4 + 8 * half))) * 16};
+  auto frag = [&](const uint8_t* from, int i, uint32_t at) { return *reinterpret_cast<const f16x8*>(from + i * kFrag + at); };
+
+  if (ntiles > 0) stage(s_page[0], 0);
+  for (int tl = 0; tl < ntiles; ++tl) {
+    const uint8_t* from = s_page[tl & 1];
+    const float2 now = sc;
+    if (tl + 1 < ntiles) {
+      load(page);
+      page = table[min(tl + 2, ntiles - 1)];
     }
-  };
-  auto attend = [&](Raw& w, int tl) {
-    f32x16 S[2];
+    __syncthreads();
+    const bool works = tl < mine;
+    f16x8 ph[4], pl[4];
+    if (works) {
+      f32x16 S[2];
 #pragma unroll
-    for (int T = 0; T < 2; ++T) {
-      f32x16 z = {};
+      for (int T = 0; T < 2; ++T) {
+        f32x16 z = {};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f16x8 kf = halves8(w.k[T][i >> 1][2 * (i & 1)], w.k[T][i >> 1][2 * (i & 1) + 1]);
-        if (PREC > 0) z = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[i], z, 0, 0, 0);
-        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[i], z, 0, 0, 0);
-      }
-      S[T] = z;
-    }
-    const float c = score_scale(rowscale, w.sc.x);
-    const bool edge = (tl + 1) * kPage > least;
-    if (edge) {
-#pragma unroll
-      for (int T = 0; T < 2; ++T)
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (tl * kPage + 32 * T + 8 * (j >> 2) + 4 * half + (j & 3) >= r.sees) S[T][j] = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t keep = below(tl * kPage + 16 * i + 4 * (half + 2 * j), s.len);
-          w.v[0][j][i] &= keep;
-          w.v[1][j][i] &= keep;
+        for (int i = 0; i < 4; ++i) {
+          const f16x8 kf = frag(from, 4 * T + i, kfrom[i >> 1]);
+          if (PREC > 0) z = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[i], z, 0, 0, 0);
+          z = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[i], z, 0, 0, 0);
         }
-    }
-    float top = S[0][0];
+        S[T] = z;
+      }
+      const float c = score_scale(rowscale, now.x);
+      if ((tl + 1) * kPage > least) {
 #pragma unroll
-    for (int T = 0; T < 2; ++T)
+        for (int T = 0; T < 2; ++T)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) top = fmaxf(top, S[T][j]);
-    top = max_across32(top) * c;
-    if (__any(top > m + kRaise)) {
-      const float next = top > m + kRaise ? top - kTop : m;
-      const float f = __builtin_amdgcn_exp2f(m - next);
-      m = next;
-      lsum *= f;
-      O[0] *= f;
-      O[1] *= f;
-    }
-    if (w.sc.y != vscale) {
-      const float f = vscale / w.sc.y;
-      vscale = w.sc.y;
-      O[0] *= f;
-      O[1] *= f;
-    }
+          for (int j = 0; j < 16; ++j)
+            if (tl * kPage + 32 * T + 8 * (j >> 2) + 4 * half + (j & 3) >= r.sees) S[T][j] = -INFINITY;
+      }
+      float top = S[0][0];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      f16x8 ph, pl;
+      for (int T = 0; T < 2; ++T)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(S[u >> 1][8 * (u & 1) + j], c, -m));
-        lsum += p;
-        ph[j] = (_Float16)p;
-        if (PREC > 1) pl[j] = (_Float16)(p - (float)ph[j]);
+        for (int j = 0; j < 16; j += 2) top = largest(largest(top, S[T][j]), S[T][j + 1]);
+      top = max_across32(top) * c;
+      if (__any(top > m + kRaise)) {
+        const float next = top > m + kRaise ? top - kTop : m;
+        const float f = __builtin_amdgcn_exp2f(m - next);
+        m = next;
+        lsum *= f;
+        O[0] *= f;
+        O[1] *= f;
+      }
+      if (now.y != vscale) {
+        const float f = vscale / now.y;
+        vscale = now.y;
+        O[0] *= f;
+        O[1] *= f;
       }
 #pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        const f16x8 vf = halves8(w.v[d][0][u], w.v[d][1][u]);
-        if (PREC > 1) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl, O[d], 0, 0, 0);
-        O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph, O[d], 0, 0, 0);
+      for (int u = 0; u < 4; ++u) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(S[u >> 1][8 * (u & 1) + j], c, -m));
+          ph[u][j] = (_Float16)p;
+          if (PREC > 1) {
+            lsum += p;
+            pl[u][j] = (_Float16)(p - (float)ph[u][j]);
+          }
+        }
+        if (PREC < 2) {            // (the sum of the weights as they are used)
+#pragma unroll
+          for (int j = 0; j < 8; j += 2)
+            lsum = __builtin_amdgcn_fdot2(half2_of(ph[u][j], ph[u][j + 1]), half2_of((_Float16)1.0f, (_Float16)1.0f), lsum, false);
+        }
       }
     }
-  };
-  if (ntiles > 0) {
-    Raw cur, next;
-    load(cur, 0);
-    for (int tl = 0; tl < ntiles; ++tl) {
-      if (tl + 1 < ntiles) load(next, tl + 1);
-      attend(cur, tl);
-      cur = next;
+    if (tl + 1 < ntiles) stage(s_page[(tl + 1) & 1], tl + 1);
+    if (works) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          const f16x8 vf = frag(from, 8 + 4 * d + u, lane * 16);
+          if (PREC > 1) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl[u], O[d], 0, 0, 0);
+          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[u], O[d], 0, 0, 0);
+        }
     }
   }
   lsum += __shfl_xor(lsum, 32, 64);
