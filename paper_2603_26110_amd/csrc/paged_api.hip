@@ -191,7 +191,8 @@ tq_status tqp_attend(const tqp_params* params, const tqp_cache* cache, const tqp
   if (unit_rows >= ((int64_t)1 << 30) || (int64_t)rows * group >= ((int64_t)1 << 30) || units0 >= ((int64_t)1 << 30))
     return fail(TQ_ERR_ARG, "too many rows or units for one call");
   const tqp::AttendPlan plan = tqp::plan_attend(units0, unit_rows, max_len);
-  if (plan.units * plan.nsplit >= ((int64_t)1 << 31) - 8) return fail(TQ_ERR_ARG, "grid too large");
+  // (the grid is padded by up to seven units)
+  if ((plan.units + 8 * (int64_t)plan.tiles) * plan.nsplit >= ((int64_t)1 << 31)) return fail(TQ_ERR_ARG, "grid too large");
   if (plan.workspace > 0) {
     if (!workspace) return fail(TQ_ERR_CAPACITY, "workspace of %zu bytes required", plan.workspace);
     if (workspace_bytes < plan.workspace)

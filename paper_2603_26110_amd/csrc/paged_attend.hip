@@ -30,8 +30,7 @@ namespace {
 
 constexpr int kRowsFew = 16, kRowsMany = 32;
 constexpr int kMaxSplit = 64;
-constexpr int kPartRow = kDim + 2;                    // m, l, o[64] of a row
-constexpr int kPart = kRowsFew * kPartRow;            // floats of a block's partial
+constexpr int kPartRow = kDim + 4;                    // o[64], m, l of a row of a partial (16-byte aligned)
 // The largest weight is kept between 2^7 and 2^15: the reference of the exponents
 // is 7 below the running maximum and moves when a score is 15 above it. So
 // rescaling is rare, and the steps that fp16 has at its lower end, 2^-24, are
@@ -40,12 +39,12 @@ constexpr float kTop = 7.0f, kRaise = 15.0f;
 
 __device__ __forceinline__ float lowest() { return -3.40282347e38f; }
 
-// Eight codes as fp16.
-__device__ __forceinline__ f16x8 halves8(uint32_t lo, uint32_t hi) {
-  const u32x4 w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true))};
+// Eight codes as fp16, times a power of two.
+__device__ __forceinline__ f16x8 halves8(uint32_t lo, uint32_t hi, float by = 1.0f) {
+  const u32x4 w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, by, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, by, true)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, by, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, by, true))};
   return __builtin_bit_cast(f16x8, w);
 }
 
@@ -109,6 +108,42 @@ __device__ void refuse(const AttendArgs& a, const Sequence& s, int l, int h) {
   for (int64_t i = threadIdx.x; i < (int64_t)s.n * width; i += blockDim.x)
     store_one<IO>(a, (((int64_t)l * a.rows + s.row0 + i / width) * a.heads + (int64_t)h * a.group) * kDim + i % width,
                   __builtin_nanf(""));
+}
+
+// A block's unit (layer, sequence, key/value head), row tile and split. Blocks go
+// to the XCDs in turn. A unit's blocks read the same keys and values, so all are
+// on one XCD (by its L2), and neighbouring units are on different ones, so that
+// no XCD has all of the long sequences. With fewer than eight units for each
+// XCD that do not come out even, blocks are dealt out one by one instead.
+// spread: a unit's blocks lie apart in the order (one row tile of all of an
+// XCD's units after the other: the longest of all sequences are begun first);
+// else they follow each other, while the unit's keys and values are in the L2.
+struct Place {
+  int unit, tile, split;
+  int l, b, h;
+  bool there;
+};
+
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const AttendGrid& g) {
+  const int id = blockIdx.x;
+  Place p;
+  int rest;                      // tile * nsplit + split
+  if (g.by_xcd) {
+    const int xcd = id % kXcds, j = id / kXcds, lines = (g.units + kXcds - 1) / kXcds;
+    const int line = g.spread ? j % lines : j / (g.tiles * a.nsplit);
+    rest = g.spread ? j / lines : j - line * (g.tiles * a.nsplit);
+    p.unit = line * kXcds + xcd;
+  } else {
+    p.unit = id % g.units;
+    rest = id / g.units;
+  }
+  p.there = p.unit < g.units;
+  p.split = rest % a.nsplit;
+  p.tile = rest / a.nsplit;
+  p.h = p.unit % a.kv_heads;
+  p.b = p.unit / a.kv_heads % a.B;
+  p.l = p.unit / a.kv_heads / a.B;
+  return p;
 }
 
 // A query row: its place and how many tokens it sees.
@@ -239,19 +274,84 @@ __device__ __forceinline__ uint32_t below(int first, int len) {
   return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
 }
 
+// Four dimensions of a row's result, o / l.
+template <int IO>
+__device__ __forceinline__ void store_result(const AttendArgs& a, const Sequence& s, int l, int h, int f, int d, f32x4 o, float sum) {
+  const Row x = row_of(a, s, h, f);
+  const float by = !x.fine ? __builtin_nanf("") : sum == 0.0f ? 0.0f : 1.0f / sum;
+  store_four<IO>(a, (((int64_t)l * a.rows + x.row) * a.heads + x.head) * kDim + d, o[0] * by, o[1] * by, o[2] * by, o[3] * by);
+}
+
+__device__ __forceinline__ float* part_of(const AttendArgs& a, int unit, int split, int rows_most) {
+  return a.partials + ((int64_t)unit * a.nsplit + split) * rows_most * kPartRow;
+}
+
+// Joins a unit's partials in the order of the splits. They are stored past the
+// caches of the XCDs; once they are there the block counts itself in, and the
+// last one to do so drops what its caches may hold of them, joins them all and
+// leaves the counter zero. All threads of the block come here.
+template <int IO, int ROWS>
+__device__ void join_parts(const AttendArgs& a, const Sequence& s, int l, int h, int f0, int rows, int unit, int parts,
+                           float* lds, int* s_last) {
+  const int t = threadIdx.x, threads = blockDim.x;
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (t == 0)
+    *s_last = __hip_atomic_fetch_add(a.counters + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)parts - 1;
+  __syncthreads();
+  if (!*s_last) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  const float* base = part_of(a, unit, 0, ROWS);
+  float* s_m = lds;              // [row][split]
+  float* s_l = lds + ROWS * kMaxSplit;
+  for (int e = t; e < rows * parts; e += threads) {
+    const int q = e / parts, p = e - q * parts;
+    const float* src = base + (int64_t)p * ROWS * kPartRow + q * kPartRow + kDim;
+    s_m[q * kMaxSplit + p] = src[0];
+    s_l[q * kMaxSplit + p] = src[1];
+  }
+  __syncthreads();
+  for (int e = t; e < rows * (kDim / 4); e += threads) {
+    const int q = e / (kDim / 4), d = e % (kDim / 4) * 4;
+    float M = lowest(), L = 0.0f;
+    f32x4 o = {};
+    for (int p = 0; p < parts; ++p) M = fmaxf(M, s_m[q * kMaxSplit + p]);
+    const float* src = base + q * kPartRow + d;
+    for (int p0 = 0; p0 < parts; p0 += 8) {
+      f32x4 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[j] = *reinterpret_cast<const f32x4*>(src + (int64_t)min(p0 + j, parts - 1) * ROWS * kPartRow);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (p0 + j >= parts) break;
+        const float f = __builtin_amdgcn_exp2f(s_m[q * kMaxSplit + p0 + j] - M);
+        L += s_l[q * kMaxSplit + p0 + j] * f;
+        o += v[j] * f;
+      }
+    }
+    store_result<IO>(a, s, l, h, f0 + q, d, o, L);
+  }
+  if (t == 0) __hip_atomic_store(a.counters + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ void store_part(float* p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void store_part(float* p, f32x4 x) {
+  asm volatile("global_store_dwordx4 %0, %1, off sc1" ::"v"(p), "v"(x) : "memory");   // (as the store above, four at a time)
+}
+
 // ------------------------------------------------------------- few rows
 template <int IO, int PREC, int ROPE, int W>
-__global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendArgs a, int total, int per_xcd, int tiles) {
+__global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendArgs a, AttendGrid grid) {
   constexpr int kStride = kDim + 4;
   __shared__ float s_m[W][kRowsFew], s_l[W][kRowsFew];
+  static_assert(W * kStride >= 2 * kMaxSplit, "room for the splits' statistics");
   __shared__ __align__(16) float s_o[W * kRowsFew * kStride];
   __shared__ int s_last;
-  // Blocks go to the XCDs in turn; a unit's blocks are neighbours on one.
-  const int work = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
-  if (work >= total) return;
-  const int unit = work / a.nsplit, split = work - unit * a.nsplit;
-  const int tile = unit % tiles, rest = unit / tiles;
-  const int h = rest % a.kv_heads, b = (rest / a.kv_heads) % a.B, l = rest / a.kv_heads / a.B;
+  const Place place = place_of(a, grid);
+  if (!place.there) return;
+  const int l = place.l, b = place.b, h = place.h, tile = place.tile, split = place.split;
+  const int unit = place.unit * grid.tiles + tile;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, g = lane >> 4, c16 = lane & 15;
   const Sequence s = sequence_of(a, b);
   // The table's entries of the pages that the wave starts with, where that does
@@ -438,96 +538,65 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
     *reinterpret_cast<f32x4*>(s_o + (wave * kRowsFew + c16) * kStride + 16 * d + 4 * g) = O[d] * vscale;
   __syncthreads();
 
-  float* part = a.partials + ((int64_t)unit * a.nsplit + split) * kPart;
-  for (int e = t; e < rows * kDim; e += W * 64) {
-    const int q = e / kDim, d = e % kDim;
-    float M = lowest(), L = 0.0f, o = 0.0f;
+  float* part = parts > 1 ? part_of(a, unit, split, kRowsFew) : nullptr;
+  for (int e = t; e < rows * (kDim / 4); e += W * 64) {
+    const int q = e / (kDim / 4), d = e % (kDim / 4) * 4;
+    float M = lowest(), L = 0.0f;
+    f32x4 o = {};
 #pragma unroll
     for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[w][q]);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float f = __builtin_amdgcn_exp2f(s_m[w][q] - M);
       L += s_l[w][q] * f;
-      o += s_o[(w * kRowsFew + q) * kStride + d] * f;
+      o += *reinterpret_cast<const f32x4*>(s_o + (w * kRowsFew + q) * kStride + d) * f;
     }
     if (parts > 1) {
-      __hip_atomic_store(part + q * kPartRow + 2 + d, o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      store_part(part + q * kPartRow + d, o);
       if (d == 0) {
-        __hip_atomic_store(part + q * kPartRow, M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(part + q * kPartRow + 1, L, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        store_part(part + q * kPartRow + kDim, M);
+        store_part(part + q * kPartRow + kDim + 1, L);
       }
     } else {
-      const Row x = row_of(a, s, h, f0 + q);
-      store_one<IO>(a, (((int64_t)l * a.rows + x.row) * a.heads + x.head) * kDim + d,
-                    !x.fine ? __builtin_nanf("") : L == 0.0f ? 0.0f : o / L);
+      store_result<IO>(a, s, l, h, f0 + q, d, o, L);
     }
   }
   if (parts == 1) return;
 
-  // The partials are stored past the caches of the XCDs; once they are there
-  // this block counts itself in, and the last one to do so joins them all.
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-  if (t == 0)
-    s_last = __hip_atomic_fetch_add(a.counters + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)parts - 1;
-  __syncthreads();
-  if (!s_last) return;
-  const float* base = a.partials + (int64_t)unit * a.nsplit * kPart;
-  float* s_f = s_o;              // [row][part] weights (16 x 64 at most)
-  float* s_lp = s_o + kRowsFew * kMaxSplit;
-  static_assert(W * kRowsFew * kStride >= 2 * kRowsFew * kMaxSplit, "room for the weights");
-  for (int e = t; e < rows * parts; e += W * 64) {
-    const int q = e / parts, p = e - q * parts;
-    s_f[q * kMaxSplit + p] = __hip_atomic_load(base + (int64_t)p * kPart + q * kPartRow, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_lp[q * kMaxSplit + p] = __hip_atomic_load(base + (int64_t)p * kPart + q * kPartRow + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  for (int e = t; e < rows * kDim; e += W * 64) {
-    const int q = e / kDim, d = e % kDim;
-    float M = lowest(), L = 0.0f, o = 0.0f;
-    for (int p = 0; p < parts; ++p) M = fmaxf(M, s_f[q * kMaxSplit + p]);
-    const float* src = base + q * kPartRow + 2 + d;
-    for (int p0 = 0; p0 < parts; p0 += 8) {
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        v[j] = __hip_atomic_load(src + (int64_t)min(p0 + j, parts - 1) * kPart, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (p0 + j >= parts) break;
-        const float f = __builtin_amdgcn_exp2f(s_f[q * kMaxSplit + p0 + j] - M);
-        L += s_lp[q * kMaxSplit + p0 + j] * f;
-        o += v[j] * f;
-      }
-    }
-    const Row x = row_of(a, s, h, f0 + q);
-    store_one<IO>(a, (((int64_t)l * a.rows + x.row) * a.heads + x.head) * kDim + d,
-                  !x.fine ? __builtin_nanf("") : L == 0.0f ? 0.0f : o / L);
-  }
-  if (t == 0) __hip_atomic_store(a.counters + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  join_parts<IO, kRowsFew>(a, s, l, h, f0, rows, unit, parts, s_o, &s_last);
 }
 
 // ------------------------------------------------------------ many rows
-// Four waves of 32 rows share a page: each thread loads 16 bytes of its keys and
-// values, converts them to fp16 and leaves them in LDS as the matrix
-// instructions take them (16 bytes a lane, read without conflicts). While one
-// page is worked on the next one's codes are on their way in registers, and one
-// barrier a page is enough for two buffers. Conversions and loads so cost a
-// quarter of what they would with a page per wave; what remains is bound by the
-// vector unit: per score one exponential (quarter rate), a multiply-add, half a
-// maximum, half a conversion and half a sum.
+// The waves of a group, 32 rows each, share a page: their threads load its codes,
+// convert them to fp16 and leave them in LDS as the matrix instructions take
+// them (16 bytes a lane, read without conflicts). While one page is worked on
+// the next one's codes are on their way in registers, and one barrier a page is
+// enough for two buffers. Conversions and loads so cost a quarter (half) of what
+// they would with a page per wave; what remains is bound by the vector unit: per
+// score one exponential (quarter rate), a multiply-add, half a maximum, half a
+// conversion and half a sum.
+//
+// GROUPS: 1: one group of four waves, 128 rows a block. 2: two groups of two
+// waves, 64 rows a block, that take every other page each and are joined at the
+// end: twice the blocks and half the pages one after the other, for calls that
+// do not fill the chip.
+//
+// Values are converted over the reference scale of the output's sums, times the
+// power of two by which the page's scale differs (fp16 holds 448 * 2^6 and the
+// steps of 2^-9 * 2^-6); the sums move to another reference only where it
+// differs by more.
 constexpr int kFrag = 64 * 16;                        // bytes of an operand of one instruction
 
-template <int IO, int PREC, int ROPE>
-__global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, int per_xcd, int tiles) {
-  // [buffer][keys: 32-token half T, step | values: 32-dimension half, step][lane]
-  __shared__ __align__(16) uint8_t s_page[2][16 * kFrag];
+template <int IO, int PREC, int ROPE, int GROUPS>
+__global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid grid) {
+  constexpr int kWaves = 4 / GROUPS, kThreads = 64 * kWaves;   // of a group
+  // [group][buffer][keys: 32-token half T, step | values: 32-dimension half, step][lane]
+  __shared__ __align__(16) uint8_t s_page[GROUPS][2][16 * kFrag];
   __shared__ int s_most[4];
-  const int work = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
-  if (work >= total) return;
+  const Place place = place_of(a, grid);
+  if (!place.there) return;
   // (the last rows first: under a causal mask they see the most)
-  const int tile = tiles - 1 - work % tiles, rest = work / tiles;
-  const int h = rest % a.kv_heads, b = (rest / a.kv_heads) % a.B, l = rest / a.kv_heads / a.B;
+  const int l = place.l, b = place.b, h = place.h, tile = grid.tiles - 1 - place.tile;
   const int lane = threadIdx.x & 63, half = lane >> 5, c32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Sequence s = sequence_of(a, b);
@@ -536,8 +605,9 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
     if (tile == 0) refuse<IO>(a, s, l, h);
     return;
   }
-  if (tile * 4 * kRowsMany >= s.n * a.group) return;
-  const int f0 = (tile * 4 + wave) * kRowsMany;
+  if (tile * kWaves * kRowsMany >= s.n * a.group) return;
+  const int group = wave / kWaves;
+  const int f0 = (tile * kWaves + wave % kWaves) * kRowsMany;
   const Row r = row_of(a, s, h, f0 + c32);
   int most = r.sees, least = r.fine ? r.sees : INT_MAX;
 #pragma unroll
@@ -550,7 +620,16 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
   if (lane == 0) s_most[wave] = most;
   __syncthreads();
   const int mine = (most + kPage - 1) / kPage;        // pages that the wave's rows see, and the block's
-  const int ntiles = (__builtin_amdgcn_readfirstlane(max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]))) + kPage - 1) / kPage;
+  const int all = (__builtin_amdgcn_readfirstlane(max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]))) + kPage - 1) / kPage;
+  // The block's pages [first, ntiles) of these (splits only with two groups).
+  int parts = 1, first = 0, ntiles = all;
+  if (GROUPS == 2 && a.nsplit > 1) {
+    const int st = max((all + a.nsplit - 1) / a.nsplit, 4);
+    parts = max((all + st - 1) / st, 1);
+    if (place.split >= parts) return;
+    first = place.split * st;
+    ntiles = min(all, first + st);
+  }
 
   const int64_t region = ((int64_t)(a.layer0 + l) * a.kv_heads + h) * a.cache.pages;
   const uint8_t* kplane = a.cache.k + region * kPageBytes;
@@ -558,46 +637,71 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
   const float2* scales = reinterpret_cast<const float2*>(a.cache.scales) + region;
   const int32_t* table = a.table + (int64_t)b * a.width;
 
-  // A thread's part of a page: 16 dimensions of a token's key (token
-  // threadIdx/4, dimensions 16 (threadIdx%4) ..), 16 tokens of a dimension's
-  // value (group `wave`, dimension `lane`).
-  u32x4 kw, vw;
+  // A thread's part of a page, GROUPS times: 16 dimensions of a token's key
+  // (token tok, dimensions 16 cc ..), 16 tokens of a dimension's value (token
+  // group vg, dimension vd).
+  const int tg = threadIdx.x % kThreads;
+  u32x4 kw[GROUPS], vw[GROUPS];
   float2 sc = make_float2(1.0f, 1.0f);
   auto load = [&](int page) {
     const bool bad = page < 0 || page >= a.cache.pages;
     page = bad ? 0 : page;
-    kw = *reinterpret_cast<const u32x4*>(kplane + (int64_t)page * kPageBytes + threadIdx.x * 16);
-    vw = *reinterpret_cast<const u32x4*>(vplane + (int64_t)page * kPageBytes + threadIdx.x * 16);
+    const u32x4* kp = reinterpret_cast<const u32x4*>(kplane + (int64_t)page * kPageBytes) + tg;
+    const u32x4* vp = reinterpret_cast<const u32x4*>(vplane + (int64_t)page * kPageBytes) + tg;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      kw[i] = kp[i * kThreads];
+      vw[i] = vp[i * kThreads];
+    }
     sc = scales[page];
-    if (bad) kw = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+    if (bad) {
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) kw[i] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+    }
   };
   // Key operands: step i, lane (half, token): dimensions 32 half + 8 i .. +7.
   // (the token's place within an operand is turned by what the four threads of
   // a token differ in, so that their stores go to different banks)
-  const int tok = threadIdx.x >> 2, cc = threadIdx.x & 3;
-  const uint32_t kto = ((tok >> 5) * 4 + 2 * (cc & 1)) * kFrag + ((cc >> 1) * 32 + ((tok & 31) ^ (4 * (cc & 1) + 8 * (cc >> 1)))) * 16;
   // Value operands: step u, lane (half, dimension): tokens 16 u + 4 half + r and
   // 16 u + 8 + 4 half + r.
-  const uint32_t vto = (8 + (lane >> 5) * 4) * kFrag + ((wave & 1) * 32 + c32) * 16 + (wave >> 1) * 8;
+  uint32_t kto[GROUPS], vto[GROUPS];
+  int vg[GROUPS];
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const int at = tg + i * kThreads, tok = at >> 2, cc = at & 3, vd = at & 63;
+    vg[i] = at >> 6;
+    kto[i] = ((tok >> 5) * 4 + 2 * (cc & 1)) * kFrag + ((cc >> 1) * 32 + ((tok & 31) ^ (4 * (cc & 1) + 8 * (cc >> 1)))) * 16;
+    vto[i] = (8 + (vd >> 5) * 4) * kFrag + ((vg[i] & 1) * 32 + (vd & 31)) * 16 + (vg[i] >> 1) * 8;
+  }
+  // The reference scale of the page that is staged, and what sums over the one
+  // before are multiplied by to get there.
+  float vscale = 0.0f, moved = 1.0f;
   auto stage = [&](uint8_t* to, int tl) {
-    *reinterpret_cast<f16x8*>(to + kto) = halves8(kw[0], kw[1]);
-    *reinterpret_cast<f16x8*>(to + kto + kFrag) = halves8(kw[2], kw[3]);
-    if ((tl + 1) * kPage > s.len) {
+    const float by = sc.y / vscale;
+    const bool near = by >= 0.015625f && by <= 64.0f;   // (uniform)
+    moved = near ? 1.0f : vscale / sc.y;
+    vscale = near ? vscale : sc.y;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vw[i] &= below(tl * kPage + 16 * i + 4 * wave, s.len);
-    }
+    for (int j = 0; j < GROUPS; ++j) {
+      *reinterpret_cast<f16x8*>(to + kto[j]) = halves8(kw[j][0], kw[j][1]);
+      *reinterpret_cast<f16x8*>(to + kto[j] + kFrag) = halves8(kw[j][2], kw[j][3]);
+      if ((tl + 1) * kPage > s.len) {
 #pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-      const f16x8 v = halves8(vw[i], vw[i + 1]);
-      const u32x4 w = __builtin_bit_cast(u32x4, v);
-      *reinterpret_cast<u32x2*>(to + vto + i * kFrag) = u32x2{w[0], w[1]};
-      *reinterpret_cast<u32x2*>(to + vto + (i + 1) * kFrag) = u32x2{w[2], w[3]};
+        for (int i = 0; i < 4; ++i) vw[j][i] &= below(tl * kPage + 16 * i + 4 * vg[j], s.len);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const u32x4 w = __builtin_bit_cast(u32x4, halves8(vw[j][i], vw[j][i + 1], near ? by : 1.0f));
+        *reinterpret_cast<u32x2*>(to + vto[j] + i * kFrag) = u32x2{w[0], w[1]};
+        *reinterpret_cast<u32x2*>(to + vto[j] + (i + 1) * kFrag) = u32x2{w[2], w[3]};
+      }
     }
   };
   int page = 0;                  // table entry of the page to load next
-  if (ntiles > 0) {
-    load(table[0]);
-    page = table[min(1, ntiles - 1)];
+  const int begin = first + group;
+  if (begin < ntiles) {
+    load(table[begin]);
+    page = table[min(begin + GROUPS, ntiles - 1)];
   }
 
   // q': lane (half, column) has dimensions 32 half .. +31 of its row
@@ -618,21 +722,23 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
     rowscale = a.scale2 * pow2(max(e, -126));
   }
 
-  float m = lowest(), lsum = 0.0f, vscale = 1.0f;
+  float m = lowest(), lsum = 0.0f, scale = 0.0f;   // scale: the reference that O is over
   f32x16 O[2] = {};
   const uint32_t kfrom[2] = {(uint32_t)(32 * half + (c32 ^ (8 * half))) * 16, (uint32_t)(32 * half + (c32 ^ (4 + 8 * half))) * 16};
   auto frag = [&](const uint8_t* from, int i, uint32_t at) { return *reinterpret_cast<const f16x8*>(from + i * kFrag + at); };
 
-  if (ntiles > 0) stage(s_page[0], 0);
-  for (int tl = 0; tl < ntiles; ++tl) {
-    const uint8_t* from = s_page[tl & 1];
-    const float2 now = sc;
-    if (tl + 1 < ntiles) {
+  if (begin < ntiles) stage(s_page[group][0], begin);
+  int buffer = 0;
+  for (int tl = begin; tl < ntiles + group; tl += GROUPS, buffer ^= 1) {   // (the same turns for all groups)
+    const uint8_t* from = s_page[group][buffer];
+    const float kscale = sc.x, move = moved, over = vscale;
+    const bool more = tl + GROUPS < ntiles;
+    if (more) {
       load(page);
-      page = table[min(tl + 2, ntiles - 1)];
+      page = table[min(tl + 2 * GROUPS, ntiles - 1)];
     }
     __syncthreads();
-    const bool works = tl < mine;
+    const bool works = tl < min(mine, ntiles);
     f16x8 ph[4], pl[4];
     if (works) {
       f32x16 S[2];
@@ -647,7 +753,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
         }
         S[T] = z;
       }
-      const float c = score_scale(rowscale, now.x);
+      const float c = score_scale(rowscale, kscale);
       if ((tl + 1) * kPage > least) {
 #pragma unroll
         for (int T = 0; T < 2; ++T)
@@ -669,11 +775,10 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
         O[0] *= f;
         O[1] *= f;
       }
-      if (now.y != vscale) {
-        const float f = vscale / now.y;
-        vscale = now.y;
-        O[0] *= f;
-        O[1] *= f;
+      scale = over;
+      if (move != 1.0f) {          // (uniform)
+        O[0] *= move;
+        O[1] *= move;
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -693,7 +798,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
         }
       }
     }
-    if (tl + 1 < ntiles) stage(s_page[(tl + 1) & 1], tl + 1);
+    if (more) stage(s_page[group][buffer ^ 1], tl + GROUPS);
     if (works) {
 #pragma unroll
       for (int u = 0; u < 4; ++u)
@@ -706,8 +811,45 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
     }
   }
   lsum += __shfl_xor(lsum, 32, 64);
+  if constexpr (GROUPS == 2) {
+    // the second group's sums, by dimension, row in a lane: [wave][d, m, l][lane]
+    float* part = reinterpret_cast<float*>(s_page) + (wave % kWaves) * 34 * 64 + lane;
+    __syncthreads();
+    if (group == 1) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) part[i * 64] = O[i >> 4][i & 15] * scale;
+      part[32 * 64] = m;
+      part[33 * 64] = lsum;
+    }
+    __syncthreads();
+    if (group == 1 && parts == 1) return;
+    const float other = part[32 * 64], M = fmaxf(m, other);
+    const float f = __builtin_amdgcn_exp2f(m - M) * scale, g = __builtin_amdgcn_exp2f(other - M);
+    lsum = lsum * __builtin_amdgcn_exp2f(m - M) + part[33 * 64] * g;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) O[i >> 4][i & 15] = O[i >> 4][i & 15] * f + part[i * 64] * g;
+    scale = 1.0f;
+    if (parts > 1) {
+      const int rows = min(s.n * a.group - tile * kWaves * kRowsMany, kWaves * kRowsMany), unit = place.unit * grid.tiles + tile;
+      if (group == 0 && r.there) {
+        float* to = part_of(a, unit, place.split, kWaves * kRowsMany) + (wave * kRowsMany + c32) * kPartRow;
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            store_part(to + 32 * d + 8 * i + 4 * half, f32x4{O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]});
+        if (half == 0) {
+          store_part(to + kDim, M);
+          store_part(to + kDim + 1, lsum);
+        }
+      }
+      __shared__ int s_last;
+      join_parts<IO, kWaves * kRowsMany>(a, s, l, h, tile * kWaves * kRowsMany, rows, unit, parts, reinterpret_cast<float*>(s_page), &s_last);
+      return;
+    }
+  }
   if (!r.there) return;
-  const float f = !r.fine ? __builtin_nanf("") : lsum == 0.0f ? 0.0f : vscale / lsum;
+  const float f = !r.fine ? __builtin_nanf("") : lsum == 0.0f ? 0.0f : scale / lsum;
   const int64_t at = (((int64_t)l * a.rows + r.row) * a.heads + r.head) * kDim + 4 * half;
 #pragma unroll
   for (int d = 0; d < 2; ++d)
@@ -721,13 +863,24 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, int total, i
 AttendPlan plan_attend(int64_t units0, int64_t rows, int max_len) {
   AttendPlan p{};
   p.few = rows <= 64;
-  const int per = p.few ? kRowsFew : 4 * kRowsMany;
+  // Blocks of 128 rows where these fill the chip three times, else of 64 (an
+  // encoder's 5280 blocks of 128 rows 350 us against 460; 640 blocks of four
+  // chunks 99 against 88, 160 of one prompt 28 against 21).
+  p.groups = units0 * ((rows + 4 * kRowsMany - 1) / (4 * kRowsMany)) < 768 ? 2 : 1;
+  const int per = p.few ? kRowsFew : 4 * kRowsMany / p.groups;
   p.tiles = (int)((rows + per - 1) / per);
   p.units = units0 * p.tiles;
   p.nsplit = 1;
   p.waves = 4;
-  if (!p.few) return p;
   const int64_t pages = std::max<int64_t>((max_len + (int64_t)kPage - 1) / kPage, 1);
+  if (!p.few) {
+    // Long sequences of few rows, as below (13 units of 126 pages 97 -> 34 us,
+    // 320 of 128 pages 94 -> 80; 320 of 16 pages would go 21 -> 39).
+    const int64_t split = std::min<int64_t>(std::min<int64_t>(640 / p.units, pages / 16), kMaxSplit);
+    if (p.groups == 2 && split > 1 && pages * (split - 1) >= 20 * split) p.nsplit = (int)split;
+    if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * (2 * kRowsMany) * kPartRow * sizeof(float);
+    return p;
+  }
   // Eight waves a block where the units leave compute units free and there are
   // pages for them (20 units of 17 pages 8.8 -> 8.2 us, 160 of 33 17.9 -> 14.4),
   // or where there are so many pages that joining the waves costs nothing (640
@@ -740,7 +893,7 @@ AttendPlan plan_attend(int64_t units0, int64_t rows, int max_len) {
   // 128 pages 23.8 -> 12.4 us; 64 units of 17 pages would go 9.4 -> 10.7).
   const int64_t split = std::min<int64_t>(std::min<int64_t>(256 / p.units, pages / 16), kMaxSplit);
   if (p.waves == 8 && split > 1 && pages * (split - 1) >= 20 * split) p.nsplit = (int)split;
-  if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * kPart * sizeof(float);
+  if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * kRowsFew * kPartRow * sizeof(float);
   return p;
 }
 
@@ -748,14 +901,23 @@ namespace {
 
 template <int IO, int PREC, int ROPE>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-  const int64_t total = p.units * p.nsplit, per_xcd = (total + kXcds - 1) / kXcds;
-  const dim3 grid((unsigned)(per_xcd * kXcds)), block(p.waves * 64);
-  if (!p.few)
-    hipLaunchKernelGGL((attend_many<IO, PREC, ROPE>), grid, block, 0, st, a, (int)total, (int)per_xcd, p.tiles);
+  AttendGrid g;
+  g.units = (int)(p.units / p.tiles);
+  g.tiles = p.tiles;
+  g.by_xcd = g.units % kXcds == 0 || g.units >= 8 * kXcds;
+  // (64 ragged prompts of 20 heads, 1280 units: 223 -> 200 us; four chunks on top
+  // of long sequences, 32 units, would go 82 -> 134)
+  g.spread = !p.few && a.causal && g.units >= 64 * kXcds;
+  const int64_t lines = g.by_xcd ? (g.units + kXcds - 1) / kXcds * kXcds : g.units;
+  const dim3 grid((unsigned)(lines * p.tiles * p.nsplit)), block(p.waves * 64);
+  if (!p.few && p.groups == 1)
+    hipLaunchKernelGGL((attend_many<IO, PREC, ROPE, 1>), grid, block, 0, st, a, g);
+  else if (!p.few)
+    hipLaunchKernelGGL((attend_many<IO, PREC, ROPE, 2>), grid, block, 0, st, a, g);
   else if (p.waves == 8)
-    hipLaunchKernelGGL((attend_few<IO, PREC, ROPE, 8>), grid, block, 0, st, a, (int)total, (int)per_xcd, p.tiles);
+    hipLaunchKernelGGL((attend_few<IO, PREC, ROPE, 8>), grid, block, 0, st, a, g);
   else
-    hipLaunchKernelGGL((attend_few<IO, PREC, ROPE, 4>), grid, block, 0, st, a, (int)total, (int)per_xcd, p.tiles);
+    hipLaunchKernelGGL((attend_few<IO, PREC, ROPE, 4>), grid, block, 0, st, a, g);
   return hipGetLastError();
 }
 

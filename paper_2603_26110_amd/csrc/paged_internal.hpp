@@ -91,11 +91,18 @@ hipError_t launch_assign(const AssignArgs& a, hipStream_t st);
 hipError_t launch_release(const ReleaseArgs& a, hipStream_t st);
 hipError_t launch_append(const AppendArgs& a, hipStream_t st);
 
+// The grid of tqp_attend: (layer, sequence, key/value head)s, row tiles of each,
+// and the order in which blocks take them.
+struct AttendGrid {
+  int units, tiles;
+  int by_xcd, spread;
+};
+
 // How tqp_attend runs: rows of a unit in tiles of 16 (few rows: every unit's
-// tokens shared by `waves` waves and nsplit blocks) or of 128.
+// tokens shared by `waves` waves and nsplit blocks) or of 128 / groups.
 struct AttendPlan {
   bool few;
-  int waves, nsplit, tiles;    // tiles: row tiles of a unit
+  int waves, groups, nsplit, tiles;   // tiles: row tiles of a unit
   int64_t units;               // (layer, sequence, key/value head, row tile)
   size_t workspace;
 };
