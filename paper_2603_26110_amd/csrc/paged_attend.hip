@@ -642,7 +642,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
   // group vg, dimension vd).
   const int tg = threadIdx.x % kThreads;
   u32x4 kw[GROUPS], vw[GROUPS];
-  float2 sc = make_float2(1.0f, 1.0f);
+  float2 sc = make_float2(1.0f, 1.0f), next_sc = sc;   // of the page that is staged, and of the one on its way
   auto load = [&](int page) {
     const bool bad = page < 0 || page >= a.cache.pages;
     page = bad ? 0 : page;
@@ -653,7 +653,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
       kw[i] = kp[i * kThreads];
       vw[i] = vp[i * kThreads];
     }
-    sc = scales[page];
+    next_sc = scales[page];
     if (bad) {
 #pragma unroll
       for (int i = 0; i < GROUPS; ++i) kw[i] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
@@ -677,10 +677,17 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
   // before are multiplied by to get there.
   float vscale = 0.0f, moved = 1.0f;
   auto stage = [&](uint8_t* to, int tl) {
-    const float by = sc.y / vscale;
-    const bool near = by >= 0.015625f && by <= 64.0f;   // (uniform)
-    moved = near ? 1.0f : vscale / sc.y;
-    vscale = near ? vscale : sc.y;
+    sc.x = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(next_sc.x)));
+    sc.y = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(next_sc.y)));
+    // (scales with the same mantissa, as powers of two have, differ by a power of two)
+    const int step = __float_as_int(sc.y) - __float_as_int(vscale);
+    const bool near = (step & 0x7FFFFF) == 0 && step >= -(6 << 23) && step <= 6 << 23;   // (uniform)
+    const float by = near ? __int_as_float(step + (127 << 23)) : 1.0f;
+    moved = 1.0f;
+    if (!near) {
+      moved = vscale / sc.y;
+      vscale = sc.y;
+    }
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
       *reinterpret_cast<f16x8*>(to + kto[j]) = halves8(kw[j][0], kw[j][1]);
@@ -691,7 +698,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
       }
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
-        const u32x4 w = __builtin_bit_cast(u32x4, halves8(vw[j][i], vw[j][i + 1], near ? by : 1.0f));
+        const u32x4 w = __builtin_bit_cast(u32x4, halves8(vw[j][i], vw[j][i + 1], by));
         *reinterpret_cast<u32x2*>(to + vto[j] + i * kFrag) = u32x2{w[0], w[1]};
         *reinterpret_cast<u32x2*>(to + vto[j] + (i + 1) * kFrag) = u32x2{w[2], w[3]};
       }

@@ -35,6 +35,7 @@ __all__ = ["Params", "Cache", "PagePool", "assign", "release", "append", "attend
            "last_error", "lib_path", "PAGE", "MAX_SEQS", "ROPE_HALF", "OUT_FP32"]
 
 PAGE, MAX_SEQS = 64, 4096
+_CAPACITY = -5
 _IO = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 lib_path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libturboesm_paged.so")
@@ -98,56 +99,58 @@ def _check(status: int) -> None:
         raise TQError(f"status {status}: {last_error()}")
 
 
-def _dev(t, name: str, dtype, device=None, numel: int | None = None) -> torch.Tensor:
-    """A contiguous tensor of the type, on `device`, with at least `numel` elements."""
+# A call's marshalling is a good part of a small launch's time (9 us of host work
+# per append against 4 us of kernel, before): the checks of a call's tensors are
+# one expression, and only where that fails do they run one by one, in order, to
+# raise; structures that do not change are built with their object; the current
+# stream comes as its raw handle.
+def _dev(t, name: str, dtype, index: int | None = None, numel: int | None = None) -> torch.Tensor:
+    """A contiguous tensor of the type, on GPU `index`, with at least `numel` elements."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if index is not None and t.get_device() != index:
+        raise ValueError(f"{name} must be on GPU {index}, got {t.device}")
     if numel is not None and t.numel() < numel:
         raise ValueError(f"{name} needs {numel} entries")
     return t
 
 
-def _rows(t, name: str, dtype, nheads: int, device=None) -> _Rows:
-    """A [nlayers][rows][heads][64] tensor of any strides that the library takes."""
+def _check_rows(t, name: str, dtype, nheads: int, index: int) -> None:
+    """Raises unless t is a [nlayers][rows][heads][64] tensor of strides that the library takes."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.dim() != 4 or t.shape[3] != 64 or t.shape[2] != nheads:
         raise ValueError(f"{name} must be [nlayers][rows][{nheads}][64]")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
-    s = t.stride()
-    if s[3] != 1:
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on GPU {index}, got {t.device}")
+    if t.stride(3) != 1:
         raise ValueError(f"{name}: the elements of a head must be contiguous")
+
+
+def _rows(t, shape) -> _Rows:
+    s = t.stride()
     # (the stride of a dimension of one entry says nothing)
-    return _Rows(t.data_ptr(), *[0 if n == 1 else x for n, x in zip(t.shape[:3], s)])
+    return _Rows(t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
 
 
-class _on:
-    """The device of a call's tensors as the current one (the library launches there)."""
-
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        self.back = torch.cuda.current_device()
-        if self.back != self.index:
-            torch.cuda.set_device(self.index)
-        return _raw_stream(self.index)
-
-    def __exit__(self, *_):
-        if self.back != self.index:
-            torch.cuda.set_device(self.back)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-@dataclass
+def _launch(index: int, f, *args) -> int:
+    """f(*args, stream) with the tensors' GPU as the current one (the library launches there)."""
+    if _current_device() == index:
+        return f(*args, _raw_stream(index))
+    with torch.cuda.device(index):
+        return f(*args, _raw_stream(index))
+
+
+@dataclass(frozen=True)
 class Params:
     """Model-level parameters (tqp_params). ``rope_cs`` comes from the package's
     rope_table(); None where q and k come rotated, or the model has no RoPE."""
@@ -159,16 +162,19 @@ class Params:
     flags: int = 0
     softmax_scale: float = 0.125
 
-    def c(self, device=None) -> _Params:
+    def __post_init__(self):
         if self.io_dtype not in _IO:
             raise TypeError(f"io_dtype must be one of {[str(d) for d in _IO]}")
         cs = self.rope_cs
         if cs is not None:
-            _dev(cs, "rope_cs", torch.float32, device)
+            _dev(cs, "rope_cs", torch.float32)
             if cs.dim() != 3 or tuple(cs.shape[1:]) != (32, 2):
                 raise ValueError("rope_cs must be [positions][32][2]")
-        return _Params(64, self.num_layers, self.num_heads, self.kv_heads, _IO[self.io_dtype], self.flags,
-                       self.softmax_scale, 0 if cs is None else cs.shape[0], None if cs is None else cs.data_ptr())
+        c = _Params(64, self.num_layers, self.num_heads, self.kv_heads, _IO[self.io_dtype], self.flags,
+                    self.softmax_scale, 0 if cs is None else cs.shape[0], None if cs is None else cs.data_ptr())
+        object.__setattr__(self, "_c", c)
+        object.__setattr__(self, "_index", None if cs is None else cs.get_device())
+        object.__setattr__(self, "_out", torch.float32 if self.flags & OUT_FP32 else self.io_dtype)
 
 
 class Cache:
@@ -188,20 +194,20 @@ class Cache:
             self.k_codes, self.v_codes, self.scales = buffers
             for name, t, last in (("k_codes", self.k_codes, PAGE * 64), ("v_codes", self.v_codes, PAGE * 64),
                                   ("scales", self.scales, 2)):
-                _dev(t, name, torch.float32 if last == 2 else torch.uint8, self.k_codes.device)
+                _dev(t, name, torch.float32 if last == 2 else torch.uint8, self.k_codes.get_device())
                 if tuple(t.shape) != (*shape, last):
                     raise ValueError(f"{name} must be {[*shape, last]}")
-        self.device = self.k_codes.device
+        self.device, self._index = self.k_codes.device, self.k_codes.get_device()
+        k = self.k_codes.view(torch.float8_e4m3fn).view(*shape, PAGE, 64)
+        v = self.v_codes.view(torch.float8_e4m3fn).view(*shape, 4, 64, 4, 4).permute(0, 1, 2, 5, 3, 6, 4)
+        self._values = (k, v, self.scales)
         self._c = _Cache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.scales.data_ptr(), pages)
 
     def values(self):
         """Views of what the cache holds, as float8_e4m3fn tensors: keys [L][kv_heads][pages][64 tokens][64], values
         [L][kv_heads][pages][4][4][4][64] (token 16 i + 4 g + r at [i][g][r]), and the scales [L][kv_heads][pages][2]
         of keys and values that they are multiplied by."""
-        shape = (self.num_layers, self.kv_heads, self.pages)
-        k = self.k_codes.view(torch.float8_e4m3fn).view(*shape, PAGE, 64)
-        v = self.v_codes.view(torch.float8_e4m3fn).view(*shape, 4, 64, 4, 4).permute(0, 1, 2, 5, 3, 6, 4)
-        return k, v, self.scales
+        return self._values
 
 
 class PagePool:
@@ -213,7 +219,7 @@ class PagePool:
         self.pages = pages
         self.stack = torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device)
         self.state = torch.tensor([pages, 0, 0, 0], dtype=torch.int32, device=device)
-        self.device = self.stack.device
+        self.device, self._index = self.stack.device, self.stack.get_device()
         self._c = _Pool(self.stack.data_ptr(), self.state.data_ptr(), pages)
 
 
@@ -221,75 +227,98 @@ def cache_bytes(num_layers: int, kv_heads: int, pages: int) -> int:
     return int(_load().tqp_cache_bytes(num_layers, kv_heads, pages))
 
 
-def _pool_args(pool, table, seq_len):
-    dev = pool.device
-    _dev(table, "table", torch.int32, dev)
-    if table.dim() != 2:
-        raise ValueError("table must be [B][width]")
-    B = table.shape[0]
-    _dev(seq_len, "seq_len", torch.int32, dev, B)
-    return dev, B
+def _pool_checks(pool: PagePool, table, seq_len, other, name: str) -> int:
+    """The checks that assign and release share. Returns the number of sequences."""
+    index, i32 = pool._index, torch.int32
+    try:
+        B = table.shape[0]
+        fine = (table.dtype is i32 and seq_len.dtype is i32 and other.dtype is i32 and len(table.shape) == 2
+                and table.is_contiguous() and seq_len.is_contiguous() and other.is_contiguous()
+                and index >= 0 and table.get_device() == index and seq_len.get_device() == index
+                and other.get_device() == index and seq_len.numel() >= B and other.numel() >= B)
+    except (AttributeError, IndexError):
+        fine = False
+    if not fine:
+        _dev(table, "table", i32, index)
+        if table.dim() != 2:
+            raise ValueError("table must be [B][width]")
+        B = table.shape[0]
+        _dev(seq_len, "seq_len", i32, index, B)
+        _dev(other, name, i32, index, B)
+    return B
 
 
 def assign(pool: PagePool, table, seq_len, new_tokens, rows: int, out=None):
     """Pages and slots for the new tokens of every sequence (tqp_assign): fills ``table`` [B][width], advances
     ``seq_len`` [B], and returns (slots int64 [rows], pos int32 [rows], row0 int32 [B+1], granted int32 [B]).
     ``rows``: the rows of the packed batch, at least the sum of new_tokens. ``out``: the four tensors to write to."""
-    L = _load()
-    dev, B = _pool_args(pool, table, seq_len)
-    _dev(new_tokens, "new_tokens", torch.int32, dev, B)
+    L = _lib or _load()
+    B = _pool_checks(pool, table, seq_len, new_tokens, "new_tokens")
     rows = int(rows)
     if out is None:
-        out = (torch.empty(rows, dtype=torch.int64, device=dev), torch.empty(rows, dtype=torch.int32, device=dev),
-               torch.empty(B + 1, dtype=torch.int32, device=dev), torch.empty(B, dtype=torch.int32, device=dev))
+        dev, i32 = pool.device, torch.int32
+        out = (torch.empty(rows, dtype=torch.int64, device=dev), torch.empty(rows, dtype=i32, device=dev),
+               torch.empty(B + 1, dtype=i32, device=dev), torch.empty(B, dtype=i32, device=dev))
     else:
         for name, t, dtype, n in zip(("slots", "pos", "row0", "granted"), out,
                                      (torch.int64, torch.int32, torch.int32, torch.int32), (rows, rows, B + 1, B)):
-            _dev(t, name, dtype, dev, n)
+            _dev(t, name, dtype, pool._index, n)
     slots, pos, row0, granted = out
-    with _on(dev) as stream:
-        _check(L.tqp_assign(ctypes.byref(pool._c), table.data_ptr(), table.shape[1], B, seq_len.data_ptr(),
-                            new_tokens.data_ptr(), rows, slots.data_ptr(), pos.data_ptr(), row0.data_ptr(),
-                            granted.data_ptr(), stream))
+    _check(_launch(pool._index, L.tqp_assign, ctypes.byref(pool._c), table.data_ptr(), table.shape[1], B,
+                   seq_len.data_ptr(), new_tokens.data_ptr(), rows, slots.data_ptr(), pos.data_ptr(), row0.data_ptr(),
+                   granted.data_ptr()))
     return slots, pos, row0, granted
 
 
 def release(pool: PagePool, table, seq_len, keep) -> None:
     """Cuts every sequence to min(keep, seq_len) tokens and takes the pages it no longer needs back (tqp_release)."""
-    L = _load()
-    dev, B = _pool_args(pool, table, seq_len)
-    _dev(keep, "keep", torch.int32, dev, B)
-    with _on(dev) as stream:
-        _check(L.tqp_release(ctypes.byref(pool._c), table.data_ptr(), table.shape[1], B, seq_len.data_ptr(),
-                             keep.data_ptr(), stream))
+    L = _lib or _load()
+    B = _pool_checks(pool, table, seq_len, keep, "keep")
+    _check(_launch(pool._index, L.tqp_release, ctypes.byref(pool._c), table.data_ptr(), table.shape[1], B,
+                   seq_len.data_ptr(), keep.data_ptr()))
 
 
-def _cache_of(params: Params, cache: Cache):
+def _model_checks(params: Params, cache: Cache) -> int:
+    """The GPU of a call, once params and cache belong together."""
+    index = cache._index
     if cache.num_layers != params.num_layers or cache.kv_heads != params.kv_heads:
         raise ValueError("the cache has other layers or heads than params")
-    return ctypes.byref(cache._c)
+    if params._index is not None and params._index != index:
+        raise ValueError("rope_cs must be on the cache's GPU")
+    return index
 
 
 def append(params: Params, cache: Cache, k, v, slots, pos, layer0: int = 0) -> None:
     """Quantizes k, v [nlayers][rows][kv_heads][64] into the cache (tqp_append). ``slots`` int64 [rows] and ``pos``
     int32 [rows] come from assign(). k and v may be slices (strides in multiples of 8 elements)."""
-    L = _load()
-    dev = cache.device
-    p, c = params.c(dev), _cache_of(params, cache)
-    kr, vr = _rows(k, "k", params.io_dtype, params.kv_heads, dev), _rows(v, "v", params.io_dtype, params.kv_heads, dev)
-    if k.shape != v.shape:
-        raise ValueError("k and v must have the same shape")
-    nl, rows = k.shape[:2]
-    _dev(slots, "slots", torch.int64, dev, rows)
-    _dev(pos, "pos", torch.int32, dev, rows)
-    with _on(dev) as stream:
-        _check(L.tqp_append(ctypes.byref(p), c, ctypes.byref(kr), ctypes.byref(vr), rows, layer0, nl,
-                            slots.data_ptr(), pos.data_ptr(), stream))
+    L = _lib or _load()
+    index = _model_checks(params, cache)
+    io, heads = params.io_dtype, params.kv_heads
+    try:
+        shape = k.shape
+        rows = shape[1]
+        fine = (k.dtype is io and v.dtype is io and slots.dtype is torch.int64 and pos.dtype is torch.int32
+                and len(shape) == 4 and shape[3] == 64 and shape[2] == heads and v.shape == shape
+                and k.stride(3) == 1 and v.stride(3) == 1 and slots.is_contiguous() and pos.is_contiguous()
+                and index >= 0 and k.get_device() == index and v.get_device() == index
+                and slots.get_device() == index and pos.get_device() == index
+                and slots.numel() >= rows and pos.numel() >= rows)
+    except (AttributeError, IndexError):
+        fine = False
+    if not fine:
+        _check_rows(k, "k", io, heads, index)
+        _check_rows(v, "v", io, heads, index)
+        if k.shape != v.shape:
+            raise ValueError("k and v must have the same shape")
+        _dev(slots, "slots", torch.int64, index, rows)
+        _dev(pos, "pos", torch.int32, index, rows)
+    _check(_launch(index, L.tqp_append, ctypes.byref(params._c), ctypes.byref(cache._c), ctypes.byref(_rows(k, shape)),
+                   ctypes.byref(_rows(v, shape)), rows, layer0, shape[0], slots.data_ptr(), pos.data_ptr()))
 
 
 def workspace_bytes(params: Params, nlayers: int, B: int, max_new: int, max_len: int) -> int:
     """Bytes of the workspace that attend() needs for these sizes (0 for most)."""
-    return int(_load().tqp_workspace_bytes(ctypes.byref(params.c()), nlayers, B, max_new, max_len))
+    return int(_load().tqp_workspace_bytes(ctypes.byref(params._c), nlayers, B, max_new, max_len))
 
 
 def attend(params: Params, cache: Cache, q, pos, row0, table, seq_len, max_new: int, max_len: int, causal: bool = True,
@@ -299,40 +328,49 @@ def attend(params: Params, cache: Cache, q, pos, row0, table, seq_len, max_new: 
     ``max_len`` bound the rows and tokens of a sequence. ``workspace``: a tensor of workspace_bytes(...) bytes, zeroed
     before its first use (without one that is large enough a new one is made). Returns out
     [nlayers][rows][num_heads][64]."""
-    L = _load()
-    dev = cache.device
-    p, c = params.c(dev), _cache_of(params, cache)
-    qr = _rows(q, "q", params.io_dtype, params.num_heads, dev)
-    nl, rows = q.shape[:2]
-    _dev(table, "table", torch.int32, dev)
-    if table.dim() != 2:
-        raise ValueError("table must be [B][width]")
-    B, width = table.shape
-    _dev(pos, "pos", torch.int32, dev, rows)
-    _dev(row0, "row0", torch.int32, dev, B + 1)
-    _dev(seq_len, "seq_len", torch.int32, dev, B)
-    dtype = torch.float32 if params.flags & OUT_FP32 else params.io_dtype
+    L = _lib or _load()
+    index = _model_checks(params, cache)
+    io, heads, i32, dtype = params.io_dtype, params.num_heads, torch.int32, params._out
+    try:
+        shape = q.shape
+        rows, B = shape[1], table.shape[0]
+        fine = (q.dtype is io and len(shape) == 4 and shape[3] == 64 and shape[2] == heads and q.stride(3) == 1
+                and pos.dtype is i32 and row0.dtype is i32 and table.dtype is i32 and seq_len.dtype is i32
+                and len(table.shape) == 2 and pos.is_contiguous() and row0.is_contiguous() and table.is_contiguous()
+                and seq_len.is_contiguous() and index >= 0 and q.get_device() == index and pos.get_device() == index
+                and row0.get_device() == index and table.get_device() == index and seq_len.get_device() == index
+                and pos.numel() >= rows and row0.numel() > B and seq_len.numel() >= B)
+    except (AttributeError, IndexError):
+        fine = False
+    if not fine:
+        _check_rows(q, "q", io, heads, index)
+        _dev(table, "table", i32, index)
+        if table.dim() != 2:
+            raise ValueError("table must be [B][width]")
+        _dev(pos, "pos", i32, index, q.shape[1])
+        _dev(row0, "row0", i32, index, table.shape[0] + 1)
+        _dev(seq_len, "seq_len", i32, index, table.shape[0])
     if out is None:
-        out = torch.empty(q.shape, dtype=dtype, device=dev)
+        out = torch.empty(shape, dtype=dtype, device=cache.device)
     else:
-        _dev(out, "out", dtype, dev)
-        if out.shape != q.shape:
+        _dev(out, "out", dtype, index)
+        if out.shape != shape:
             raise ValueError("out must have the shape of q")
-    max_new, max_len = int(max_new), int(max_len)
-    pr = ctypes.byref(p)
-    need = L.tqp_workspace_bytes(pr, nl, B, max_new, max_len)
     size = 0
-    if need:
-        if workspace is not None:
-            if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or workspace.device != dev:
-                raise TypeError("workspace must be a GPU tensor on the cache's device")
-            if not workspace.is_contiguous():
-                raise ValueError("workspace must be contiguous")
-            size = workspace.numel() * workspace.element_size()
-        if size < need:
-            workspace, size = torch.zeros(need, dtype=torch.uint8, device=dev), need
-    with _on(dev) as stream:
-        _check(L.tqp_attend(pr, c, ctypes.byref(qr), rows, B, layer0, nl, pos.data_ptr(), row0.data_ptr(),
-                            table.data_ptr(), width, seq_len.data_ptr(), max_new, max_len, int(bool(causal)),
-                            out.data_ptr(), workspace.data_ptr() if need else None, size, stream))
+    if workspace is not None:
+        if not isinstance(workspace, torch.Tensor) or workspace.get_device() != index or index < 0:
+            raise TypeError("workspace must be a GPU tensor on the cache's device")
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        size = workspace.numel() * workspace.element_size()
+    args = (ctypes.byref(params._c), ctypes.byref(cache._c), ctypes.byref(_rows(q, shape)), rows, B, layer0, shape[0],
+            pos.data_ptr(), row0.data_ptr(), table.data_ptr(), table.shape[1], seq_len.data_ptr(), int(max_new),
+            int(max_len), 1 if causal else 0, out.data_ptr())
+    status = _launch(index, L.tqp_attend, *args, None if workspace is None else workspace.data_ptr(), size)
+    if status == _CAPACITY:              # (refused before anything was launched)
+        need = L.tqp_workspace_bytes(args[0], shape[0], B, int(max_new), int(max_len))
+        if need > size:
+            workspace = torch.zeros(need, dtype=torch.uint8, device=cache.device)
+            status = _launch(index, L.tqp_attend, *args, workspace.data_ptr(), need)
+    _check(status)
     return out
