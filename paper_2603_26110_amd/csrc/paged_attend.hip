@@ -938,7 +938,9 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
 
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   if (a.io == kF32) return launch<kF32, 2>(a, p, st);
-  if (a.io == kF16) return a.out_f32 ? launch<kF16, 2>(a, p, st) : launch<kF16, 1>(a, p, st);
+  if (a.io == kF16 && a.out_f32) return launch<kF16, 2>(a, p, st);
+  // (an fp16 query that is not rotated is an fp16 value as it is)
+  if (a.io == kF16) return a.cs ? launch<kF16, 1>(a, p, st) : launch<kF16, 0, kNone>(a, p, st);
   return a.out_f32 ? launch<kBF16, 2>(a, p, st) : launch<kBF16, 0>(a, p, st);
 }
 

@@ -16,6 +16,7 @@ namespace tqp {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMost = 128;       // blocks
 constexpr int kWaves = kThreads / 64;
 
 __device__ __forceinline__ int pages_of(int64_t tokens) { return (int)((tokens + kPage - 1) / kPage); }
@@ -70,20 +71,25 @@ __global__ __launch_bounds__(kThreads) void assign_kernel(AssignArgs a) {
   const int B = a.pool.B, t = threadIdx.x;
   int32_t* s_row0 = lds;                // [B + 1]
   int32_t* s_len = s_row0 + B + 1;      // [B]
-  int32_t* s_take = s_len + B;          // [B] pages taken by the requests before it; -1: not granted
+  int32_t* s_take = s_len + B;          // [B] new tokens, then pages needed, then pages taken by the
+                                        // requests before it (-1: not granted)
   __shared__ int64_t s_wave[kWaves];
   __shared__ int s_flag, s_taken;
   const int free_pages = min(max(a.pool.state[0], 0), a.pool.pages);
   const int per = (B + kThreads - 1) / kThreads, b0 = t * per, b1 = min(b0 + per, B);
   if (t == 0) s_taken = 0;
+  for (int b = t; b < B; b += kThreads) {
+    s_take[b] = a.new_tokens[b];
+    s_len[b] = a.pool.seq_len[b];
+  }
+  __syncthreads();
   int64_t n_here = 0, total;
-  for (int b = b0; b < b1; ++b) n_here += max(a.new_tokens[b], 0);
+  for (int b = b0; b < b1; ++b) n_here += max(s_take[b], 0);
   int64_t sum = scan_before(n_here, s_wave, &total);
   int64_t need_here = 0;
   for (int b = b0; b < b1; ++b) {
-    const int n = a.new_tokens[b], len = a.pool.seq_len[b];
+    const int n = s_take[b], len = s_len[b];
     s_row0[b] = (int)min(sum, (int64_t)a.rows);
-    s_len[b] = len;
     sum += max(n, 0);
     const bool valid = n >= 0 && len >= 0 && (int64_t)len + n <= (int64_t)a.pool.width * kPage && sum <= a.rows;
     const int need = valid ? pages_of((int64_t)len + n) - pages_of(len) : -1;
@@ -146,15 +152,16 @@ __global__ __launch_bounds__(kThreads) void release_kernel(ReleaseArgs a) {
   __shared__ int s_flag;
   const int free_pages = min(max(a.pool.state[0], 0), a.pool.pages);
   const int per = (B + kThreads - 1) / kThreads, b0 = t * per, b1 = min(b0 + per, B);
-  int64_t here = 0, total;
-  for (int b = b0; b < b1; ++b) {
+  for (int b = t; b < B; b += kThreads) {
     const int len = a.pool.seq_len[b];
     const bool valid = len >= 0 && len <= (int64_t)a.pool.width * kPage;
     const int kept = valid ? min(max(a.keep[b], 0), len) : -1;
     s_kept[b] = kept;
     s_first[b] = valid ? pages_of(len) - pages_of(kept) : 0;
-    here += s_first[b];
   }
+  __syncthreads();
+  int64_t here = 0, total;
+  for (int b = b0; b < b1; ++b) here += s_first[b];
   int64_t before = scan_before(here, s_wave, &total);
   for (int b = b0; b < b1; ++b) {
     const int n = s_first[b];
@@ -179,8 +186,10 @@ __global__ __launch_bounds__(kThreads) void release_kernel(ReleaseArgs a) {
 }  // namespace
 
 hipError_t launch_assign(const AssignArgs& a, hipStream_t st) {
-  // one row per thread up to a block per compute unit, then several
-  const int blocks = (int)std::min<int64_t>(std::max<int64_t>(((int64_t)a.rows + kThreads - 1) / kThreads, 1), 256);
+  // One row per thread up to a block per compute unit, then several: with fewer
+  // blocks the rows take longer (165000 rows 13 us, 128 blocks 15), with more
+  // their counting in does (1024 blocks 17).
+  const int blocks = (int)std::min<int64_t>(std::max<int64_t>(((int64_t)a.rows + kThreads - 1) / kThreads, 1), kMost);
   const size_t lds = (size_t)(3 * a.pool.B + 1) * sizeof(int32_t);
   hipLaunchKernelGGL(assign_kernel, dim3(blocks), dim3(kThreads), lds, st, a);
   return hipGetLastError();

@@ -256,9 +256,8 @@ def assign(pool: PagePool, table, seq_len, new_tokens, rows: int, out=None):
     B = _pool_checks(pool, table, seq_len, new_tokens, "new_tokens")
     rows = int(rows)
     if out is None:
-        dev, i32 = pool.device, torch.int32
-        out = (torch.empty(rows, dtype=torch.int64, device=dev), torch.empty(rows, dtype=i32, device=dev),
-               torch.empty(B + 1, dtype=i32, device=dev), torch.empty(B, dtype=i32, device=dev))
+        out = (torch.empty(rows, dtype=torch.int64, device=pool.device),
+               *torch.empty(rows + B + 1 + B, dtype=torch.int32, device=pool.device).split_with_sizes((rows, B + 1, B)))
     else:
         for name, t, dtype, n in zip(("slots", "pos", "row0", "granted"), out,
                                      (torch.int64, torch.int32, torch.int32, torch.int32), (rows, rows, B + 1, B)):
