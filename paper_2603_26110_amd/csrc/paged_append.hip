@@ -423,11 +423,11 @@ __device__ __forceinline__ Window window_of(const AppendArgs& a, int w, int lane
 }
 
 // The pages that start in the window and take one token: the next row that is
-// there has another page. (Without one in the two windows the page counts as
-// taking more, which is as right.)
-__device__ __forceinline__ uint64_t single_rows(const Window& x, int lane) {
+// there has another page. (Where that row is beyond the two windows the page
+// counts as taking more, which is as right.)
+__device__ __forceinline__ uint64_t single_rows(const AppendArgs& a, const Window& x, int lane) {
   const uint64_t above = lane == 63 ? 0 : x.v0 >> (lane + 1) << (lane + 1);
-  const bool alone = above ? (x.lead0 >> first_bit(above)) & 1 : x.v1 ? (x.lead1 >> first_bit(x.v1)) & 1 : true;
+  const bool alone = above ? (x.lead0 >> first_bit(above)) & 1 : x.v1 ? (x.lead1 >> first_bit(x.v1)) & 1 : x.t0 + 128 >= a.rows;
   return __ballot(((x.lead0 >> lane) & 1) && alone);
 }
 
@@ -615,7 +615,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int wind
   const int l = rest / windows;
   const Window x = window_of(a, rest - l * windows, lane);
   if (!x.lead0) return;
-  const uint64_t singles = single_rows(x, lane), runs = x.lead0 & ~singles;
+  const uint64_t singles = single_rows(a, x, lane), runs = x.lead0 & ~singles;
   if (runs) take_runs<IO, ROPE>(a, x, runs, l, h, s, share, lane);
   if (singles) take_singles<IO, ROPE>(a, x, singles, l, h, s, share, lane);
 }

@@ -16,7 +16,7 @@ namespace tqp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMost = 128;       // blocks
+constexpr int kMost = 256;       // blocks
 constexpr int kWaves = kThreads / 64;
 
 __device__ __forceinline__ int pages_of(int64_t tokens) { return (int)((tokens + kPage - 1) / kPage); }

@@ -591,11 +591,12 @@ def test_calls_go_to_the_current_stream():
     assert big.shape == (4096, 4096) and torch.equal(got, fine)
 
 
-@pytest.mark.parametrize("case", range(6))
+@pytest.mark.parametrize("case", range(8))
 def test_append_of_runs_in_any_form(case):
     # the same slot twice, descending slots, a page taken up again after skipped rows, across windows of rows
     slots = [[64, 64], [70] * 200, list(range(127, 63, -1)), [64, 65, -1, -1, 66, 64] + [-1] * 150 + [80, 81],
-             list(range(64, 128)) * 3 + list(range(192, 200)), [5 * 64 + t for t in (3, 4, 9, 10, 11)] * 30][case]
+             list(range(64, 128)) * 3 + list(range(192, 200)), [5 * 64 + t for t in (3, 4, 9, 10, 11)] * 30,
+             [64] + [-1] * 150 + [65], [130] + [-1] * 63 + [66] + [-1] * 63 + [67, 200]][case]
     cache = random_cache(1, 2, 6, case)
     want = ref.CacheRef(cache)
     g = torch.Generator(device=DEV).manual_seed(case)
