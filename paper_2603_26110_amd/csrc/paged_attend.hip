@@ -490,7 +490,7 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
       for (int i = 0; i < 4; ++i) O[i] *= f;
     }
     if (vs != vscale) {      // (uniform: O is in units of the page's value scale)
-      const float f = vscale / vs;
+      const float f = vscale * __builtin_amdgcn_rcpf(vs);   // (exact for powers of two)
       vscale = vs;
 #pragma unroll
       for (int i = 0; i < 4; ++i) O[i] *= f;
@@ -685,7 +685,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
     const float by = near ? __int_as_float(step + (127 << 23)) : 1.0f;
     moved = 1.0f;
     if (!near) {
-      moved = vscale / sc.y;
+      moved = vscale * __builtin_amdgcn_rcpf(sc.y);
       vscale = sc.y;
     }
 #pragma unroll
@@ -804,9 +804,6 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
             lsum = __builtin_amdgcn_fdot2(half2_of(ph[u][j], ph[u][j + 1]), half2_of((_Float16)1.0f, (_Float16)1.0f), lsum, false);
         }
       }
-    }
-    if (more) stage(s_page[group][buffer ^ 1], tl + GROUPS);
-    if (works) {
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -816,6 +813,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
           O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[u], O[d], 0, 0, 0);
         }
     }
+    if (more) stage(s_page[group][buffer ^ 1], tl + GROUPS);
   }
   lsum += __shfl_xor(lsum, 32, 64);
   if constexpr (GROUPS == 2) {
