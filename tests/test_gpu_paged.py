@@ -605,3 +605,69 @@ def test_append_of_runs_in_any_form(case):
     paged.append(paged.Params(1, 2, 2, None, F32), cache, k, v, torch.tensor(slots, device=DEV), i32([0] * len(slots)))
     want.append(k.cpu().numpy(), v.cpu().numpy(), slots, [0] * len(slots), None, False)
     same_cache(cache, want)
+
+
+def test_the_quality_command_s_paged_row():
+    from paper_2603_26110_amd import quality
+    inp = quality.inputs(heads=3, tokens=200, calib=64, seed=5)
+    got = torch.from_numpy(quality.decode_paged(inp))
+    host = ref.CacheRef(paged.Cache(1, 3, 4))
+    slots = list(range(200))
+    host.append(inp["k"][0].astype(np.float32), inp["v"][0].astype(np.float32), slots, slots, tq.rope_table(200).cpu().numpy(), False)
+    scale = 2.0 ** torch.tensor(host.e, dtype=torch.float64)
+    k, v = torch.tensor(host.k) * scale[..., 0, None, None], torch.tensor(host.v) * scale[..., 1, None, None]
+    ang = torch.arange(200, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(32, dtype=torch.float64) / 32)
+    q = torch.from_numpy(inp["q"].astype(np.float64))
+    want, spread, size = ref.attend(k, v, q, [199], [0, 1], [[0, 1, 2, 3]], [200], True, 0.125,
+                                    torch.polar(torch.ones_like(ang), ang))
+    tol = ref.bound(want, spread, size, 200, 2, F32)
+    assert bool(((got - want[0, 0]).abs() <= tol[0, 0]).all())
+
+
+def test_wrong_tensors_are_refused():
+    w = World([100, 70], [2, 1], 4, 2, seed=4)
+    slots = torch.tensor([t for t in range(w.rows)], device=DEV)
+    pool, table, lens, new = paged.PagePool(9), torch.full((2, 4), -1, dtype=torch.int32, device=DEV), i32([0, 0]), i32([2, 1])
+    kv = torch.zeros((1, w.rows, 2, 64), dtype=F16, device=DEV)
+    calls = [
+        (lambda **x: paged.assign(pool, rows=3, **x), dict(table=table, seq_len=lens, new_tokens=new)),
+        (lambda **x: paged.release(pool, **x), dict(table=table, seq_len=lens, keep=i32([0, 0]))),
+        (lambda **x: paged.append(w.params, w.cache, **x), dict(k=kv, v=kv, slots=slots, pos=i32(w.pos))),
+        (lambda **x: paged.attend(w.params, w.cache, max_new=2, max_len=100, **x),
+         dict(q=w.q, pos=i32(w.pos), row0=i32(w.row0), table=i32(w.table), seq_len=i32(w.lens))),
+    ]
+    for f, args in calls:
+        f(**args)
+        for name, t in args.items():
+            for bad in (t.cpu(), t.cpu().numpy(), None, t.double()):
+                with pytest.raises(TypeError):
+                    f(**{**args, name: bad})
+            if name not in "qkv":
+                with pytest.raises(ValueError):
+                    f(**{**args, name: torch.stack([t, t], -1)[..., 0]})
+                with pytest.raises((ValueError, TypeError)):
+                    f(**{**args, name: t.reshape(-1)[:1]})
+            else:
+                with pytest.raises(ValueError):
+                    f(**{**args, name: torch.stack([t, t], -1)[..., 0]})
+                with pytest.raises(ValueError):
+                    f(**{**args, name: t[..., :32]})
+                with pytest.raises(tq.TQError):         # (a row stride that is no multiple of 8)
+                    wide = torch.zeros((1, w.rows, t.shape[2] * 64 + 4), dtype=t.dtype, device=DEV)
+                    f(**{**args, name: wide.as_strided(t.shape, (wide.stride(0), wide.stride(1), 64, 1))})
+    f, args = calls[3]
+    for bad in (torch.empty_like(w.q, dtype=F32), torch.empty_like(w.q).cpu()):
+        with pytest.raises(TypeError):
+            f(**args, out=bad)
+    with pytest.raises(ValueError):
+        f(**args, out=torch.empty_like(w.q)[:, :1])
+    with pytest.raises(TypeError):
+        f(**args, workspace=torch.zeros(8, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        paged.append(paged.Params(1, 4, 1, None), w.cache, kv, kv, slots, i32(w.pos))
+    with pytest.raises(ValueError):
+        paged.Cache(1, 2, 3, buffers=(w.cache.k_codes, w.cache.v_codes, w.cache.scales))
+    with pytest.raises(ValueError):
+        paged.Params(1, 4, 2, torch.zeros(5, 16, 2, device=DEV))
+    with pytest.raises(TypeError):
+        paged.Params(1, 4, 2, torch.zeros(5, 32, 2))
