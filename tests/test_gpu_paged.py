@@ -671,3 +671,22 @@ def test_wrong_tensors_are_refused():
         paged.Params(1, 4, 2, torch.zeros(5, 16, 2, device=DEV))
     with pytest.raises(TypeError):
         paged.Params(1, 4, 2, torch.zeros(5, 32, 2))
+
+
+@pytest.mark.parametrize("B", [2, 64, 65, 150])
+def test_many_rows_of_many_sequences(B):
+    g = np.random.default_rng(B)
+    new = g.integers(0, 71, B).tolist()
+    new[B // 2] = 70                                    # more than 64 rows a unit
+    lens = [n + int(x) for n, x in zip(new, g.choice([0, 0, 5, 5, 90, 200], B))]
+    w = World(lens, new, 1, 1, dtype=F16, rope="pairs", seed=B, spare=1)
+    got = w.call()
+    w.check(got)
+    seq_len = list(w.lens)                              # one sequence is refused, the others stay as they are
+    seq_len[B // 2] = -5
+    again = w.call(seq_len=i32(seq_len))
+    at = slice(w.row0[B // 2], w.row0[B // 2 + 1])
+    assert bool(again[:, at].isnan().all())
+    rest = torch.ones(w.rows, dtype=torch.bool, device=DEV)
+    rest[at] = False
+    assert torch.equal(again[:, rest], got[:, rest])
