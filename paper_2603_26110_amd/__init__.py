@@ -9,6 +9,8 @@ Entry points (same names as the C ABI without the ``tq_`` prefix):
     rope_table, quantize_pack, decode_attend, decode_attend_noalloc, decode_step, dequantize,
     decode_workspace_bytes, calibrate_rotation, calibrate_lut, calibrate_ebar, set_step_wait_limit,
     cache_bytes, last_error, version
+
+The submodule ``paged`` is a paged 8-bit cache beside it (``libturboesm_paged.so``).
 """
 from __future__ import annotations
 

@@ -14,7 +14,14 @@
 // wave at a time, 16 lanes each). (One wave with a whole run took 223 registers,
 // so that few waves could wait for memory at once.)
 //
-// Bound by memory: 256 bytes of fp16 in and 128 out per token and head.
+// The least traffic is 256 bytes of fp16 in and 128 out per token and head.
+// Measured: 64 ragged prompts of up to 1024 tokens, 8 heads (119 MB) 40 us, 3
+// TB/s, bound by the latency of a block's chain of load, maximum, conversion
+// and store at four blocks a compute unit; one token of 64 sequences in 33
+// layers of 20 heads (16 MB) 23 us, bound by the lines it touches: a token's
+// value bytes of a head lie in 16 lines of 64 bytes, 46 MB written (reading
+// these lines, changing and writing them whole took 30 us); one token of one
+// layer 3.9 us.
 #include <algorithm>
 
 #include "paged_device.hpp"

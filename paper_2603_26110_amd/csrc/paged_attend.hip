@@ -17,6 +17,11 @@
 // (v_mfma_f32_16x16x32_f16), a page per wave, the waves of a block and, where
 // there are few units, several blocks share a sequence. For many rows the
 // arithmetic bounds it: 32 rows per wave (v_mfma_f32_32x32x16_f16).
+// Measured: 640 (sequence, head) of 8192 tokens (671 MB) 119 us, 5.6 TB/s, where
+// a plain read of as much takes 111; 660 of 1025 tokens 19 us; 20 of 1025 tokens
+// 9 us, a chain of latencies. Every token of 1024 with every other in 33 layers
+// of 20 heads (177 GFLOP): 310 to 340 us, up to 570 TFLOP/s (a library product
+// of 8192^3: 1168).
 //
 // Rounding: q' and the weights round to fp16 (2^-11). That is 8 times finer
 // than a bf16 output; for an fp16 output q' is taken in two parts (the error

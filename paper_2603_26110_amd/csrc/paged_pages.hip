@@ -8,6 +8,10 @@
 // by bisection in LDS. Lengths and the free count change in place, which no
 // block may do before all have read them: the block that counts itself in last
 // does it.
+//
+// Measured: 64 sequences of one new token 3.9 us (release 3.4 us); 1024
+// prompts, 168 000 rows, 13 to 14 us (release 7 us) with 256 blocks, 15 with
+// 128, 17 with 1024 (2 MB written: 0.4 us of traffic).
 #include <algorithm>
 
 #include "paged_internal.hpp"
