@@ -151,7 +151,8 @@ TQ_API tq_status tqp_release(const tqp_pool* pool, int32_t* table, int32_t table
  * is not defined (other pages are not touched).
  *
  *   k, v   device rows [nlayers][rows][kv_heads][64] of io_dtype; their
- *          row_stride is at most 2^23.
+ *          row_stride is at most 2^23. nlayers * kv_heads * ceil(rows / 64)
+ *          is less than 2^24.
  *   slots  device int64 [rows];  pos device int32 [rows] (unused and may be
  *          NULL without rope_cs).
  */
@@ -177,7 +178,10 @@ TQ_API tq_status tqp_append(const tqp_params* params, const tqp_cache* cache, co
  *   pos     device int32 [rows]; row0 device int32 [B+1];
  *   table   device int32 [B][table_width];  seq_len device int32 [B]: tokens
  *           cached, those of the rows themselves among them.
- *   max_new, max_len  host bounds on the rows and tokens of a sequence.
+ *   max_new, max_len  host bounds on the rows and tokens of a sequence. A call
+ *           whose nlayers * B * kv_heads times the row tiles of max_new (64 or
+ *           128 rows; 16 where max_new * num_heads / kv_heads <= 64) would
+ *           need 2^32 threads is refused.
  *   out     device [nlayers][rows][num_heads][64] of io_dtype, or fp32 with
  *           TQ_OUT_FP32, contiguous, 16-byte aligned.
  *   workspace device, >= tqp_workspace_bytes(...) bytes, 16-byte aligned (NULL

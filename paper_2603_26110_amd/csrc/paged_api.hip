@@ -88,6 +88,11 @@ tq_status check_pool(const tqp_pool* p, const int32_t* table, int32_t width, int
   return TQ_OK;
 }
 
+// (layer, sequence, key/value head)s and the rows of each are counted in 32 bits.
+bool too_many_units(int32_t nlayers, int32_t B, int32_t kv_heads, int64_t unit_rows) {
+  return B > (((int64_t)1 << 30) - 1) / nlayers / kv_heads || unit_rows >= ((int64_t)1 << 30);
+}
+
 tqp::Rows rows_of(const tqp_rows* r) { return tqp::Rows{r->data, r->layer_stride, r->row_stride, r->head_stride}; }
 
 tqp::CacheArgs cache_of(const tqp_cache* c) {
@@ -149,7 +154,8 @@ tq_status tqp_append(const tqp_params* params, const tqp_cache* cache, const tqp
   if (k->row_stride < 0 || k->row_stride > kMaxRowStride || v->row_stride < 0 || v->row_stride > kMaxRowStride)
     return fail(TQ_ERR_ARG, "k and v: row strides must be in [0, 2^23]");
   if (!slots || (params->rope_cs && !pos)) return fail(TQ_ERR_ARG, "a required pointer is NULL");
-  if (((int64_t)rows + 63) / 64 * nlayers * params->kv_heads >= ((int64_t)1 << 30))
+  // (a launch has fewer than 2^32 threads, 256 for the 64 rows of a layer and head)
+  if (((int64_t)rows + 63) / 64 > (((int64_t)1 << 24) - 1) / nlayers / params->kv_heads)
     return fail(TQ_ERR_ARG, "too many token-heads for one call");
   tqp::AppendArgs a{};
   a.k = rows_of(k); a.v = rows_of(v);
@@ -166,8 +172,9 @@ size_t tqp_workspace_bytes(const tqp_params* params, int32_t nlayers, int32_t B,
   if (!params || params->kv_heads <= 0 || params->num_heads < params->kv_heads || B <= 0 || nlayers <= 0 ||
       max_new <= 0 || max_len < 0)
     return 0;
-  const int64_t units = (int64_t)nlayers * B * params->kv_heads;
-  return tqp::plan_attend(units, (int64_t)max_new * (params->num_heads / params->kv_heads), max_len).workspace;
+  const int64_t unit_rows = (int64_t)max_new * (params->num_heads / params->kv_heads);
+  if (too_many_units(nlayers, B, params->kv_heads, unit_rows)) return 0;
+  return tqp::plan_attend((int64_t)nlayers * B * params->kv_heads, unit_rows, max_len).workspace;
 }
 
 tq_status tqp_attend(const tqp_params* params, const tqp_cache* cache, const tqp_rows* q, int32_t rows, int32_t B,
@@ -186,13 +193,13 @@ tq_status tqp_attend(const tqp_params* params, const tqp_cache* cache, const tqp
   if (!pos || !row0 || !table || !seq_len || !out) return fail(TQ_ERR_ARG, "a required pointer is NULL");
   if (!aligned(out, 16)) return fail(TQ_ERR_ALIGN, "out must be 16-byte aligned");
   const int group = params->num_heads / params->kv_heads;
-  const int64_t units0 = (int64_t)nlayers * B * params->kv_heads, unit_rows = (int64_t)max_new * group;
-  // (the rows of a unit and all blocks are counted in 32 bits)
-  if (unit_rows >= ((int64_t)1 << 30) || (int64_t)rows * group >= ((int64_t)1 << 30) || units0 >= ((int64_t)1 << 30))
+  const int64_t unit_rows = (int64_t)max_new * group;
+  if (too_many_units(nlayers, B, params->kv_heads, unit_rows) || (int64_t)rows * group >= ((int64_t)1 << 30))
     return fail(TQ_ERR_ARG, "too many rows or units for one call");
-  const tqp::AttendPlan plan = tqp::plan_attend(units0, unit_rows, max_len);
-  // (the grid is padded by up to seven units)
-  if ((plan.units + 8 * (int64_t)plan.tiles) * plan.nsplit >= ((int64_t)1 << 31)) return fail(TQ_ERR_ARG, "grid too large");
+  const tqp::AttendPlan plan = tqp::plan_attend((int64_t)nlayers * B * params->kv_heads, unit_rows, max_len);
+  // (a launch has fewer than 2^32 threads; the grid is padded by up to seven units)
+  if ((plan.units + 8 * (int64_t)plan.tiles) * plan.nsplit >= ((int64_t)1 << 32) / (64 * plan.waves))
+    return fail(TQ_ERR_ARG, "too many rows or units for one call");
   if (plan.workspace > 0) {
     if (!workspace) return fail(TQ_ERR_CAPACITY, "workspace of %zu bytes required", plan.workspace);
     if (workspace_bytes < plan.workspace)

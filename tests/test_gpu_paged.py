@@ -690,3 +690,25 @@ def test_many_rows_of_many_sequences(B):
     rest = torch.ones(w.rows, dtype=torch.bool, device=DEV)
     rest[at] = False
     assert torch.equal(again[:, rest], got[:, rest])
+
+
+def test_two_streams_and_one_workspace_for_all_shapes():
+    worlds = [World([5000], [1], 4, 2, seed=1), World([6000, 20], [100, 3], 2, 1, dtype=BF16, rope="half", seed=2),
+              World([3000, 2500], [2, 1], 8, 2, dtype=F32, seed=3)]
+    want = [w.call() for w in worlds]
+    need = [paged.workspace_bytes(w.params, 1, len(w.lens), max(w.new), max(w.lens)) for w in worlds]
+    assert min(need) > 0
+    room = torch.zeros(max(need), dtype=torch.uint8, device=DEV)
+    for i in (0, 1, 2, 0, 2, 1):
+        assert torch.equal(worlds[i].call(workspace=room), want[i]), i
+        assert int(room[:16384].count_nonzero()) == 0
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in worlds]
+    got = [[] for _ in worlds]
+    for _ in range(8):
+        for w, s, g in zip(worlds, streams, got):
+            with torch.cuda.stream(s):
+                g.append(w.call())
+    torch.cuda.synchronize()
+    for g, x in zip(got, want):
+        assert all(torch.equal(y, x) for y in g)

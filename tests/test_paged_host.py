@@ -144,6 +144,23 @@ def test_what_is_refused(call, kw, code, msg):
     assert msg in paged.last_error()
 
 
+@pytest.mark.parametrize("call,kw", [
+    (append, dict(rows=2 ** 31 - 1)), (append, dict(rows=2 ** 30, p=_params(kv_heads=1))),
+    (append, dict(rows=64, p=_params(num_layers=2 ** 12, num_heads=2 ** 13, kv_heads=2 ** 13), nlayers=2 ** 12)),
+    (attend, dict(B=2 ** 23)), (attend, dict(B=2 ** 15, max_new=2 ** 16)),
+    (attend, dict(B=2 ** 20, p=_params(num_heads=64, kv_heads=16), max_new=1)),
+    (attend, dict(B=2 ** 30, p=_params(num_layers=2 ** 30, num_heads=2 ** 30, kv_heads=2 ** 30), nlayers=2 ** 30)),
+])
+def test_launches_that_would_not_fit_are_refused(call, kw):
+    assert call(**kw) == -1 and "too many" in paged.last_error()
+
+
+def test_workspace_of_sizes_that_do_not_fit():
+    L, p = paged._load(), _params(num_layers=2 ** 30, num_heads=2 ** 30, kv_heads=2 ** 30)
+    assert L.tqp_workspace_bytes(ctypes.byref(p), 2 ** 30, 2 ** 30, 1, 8192) == 0
+    assert L.tqp_workspace_bytes(ctypes.byref(p), 16, 2 ** 30, 1, 8192) == 0
+
+
 def test_nothing_to_do_is_success():
     assert release(B=0, table=0, seq_len=0, keep=0) == 0
     assert append(rows=0, k=None) == 0 and append(nlayers=0) == 0
