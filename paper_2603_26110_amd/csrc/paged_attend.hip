@@ -891,8 +891,8 @@ AttendPlan plan_attend(int64_t units0, int64_t rows, int max_len) {
   AttendPlan p{};
   p.few = rows <= 64;
   // Blocks of 128 rows where these fill the chip three times, else of 64 (an
-  // encoder's 5280 blocks of 128 rows 350 us against 460; 640 blocks of four
-  // chunks 99 against 88, 160 of one prompt 28 against 21).
+  // encoder's 5280 blocks of 128 rows 346 us against 439; 640 blocks of four
+  // chunks 91 against 79, 160 of one prompt 27 against 20).
   p.groups = units0 * ((rows + 4 * kRowsMany - 1) / (4 * kRowsMany)) < 768 ? 2 : 1;
   const int per = p.few ? kRowsFew : 4 * kRowsMany / p.groups;
   p.tiles = (int)((rows + per - 1) / per);
@@ -933,7 +933,7 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   g.tiles = p.tiles;
   g.by_xcd = g.units % kXcds == 0 || g.units >= 8 * kXcds;
   // (64 ragged prompts of 20 heads, 1280 units: 223 -> 200 us; four chunks on top
-  // of long sequences, 32 units, would go 82 -> 134)
+  // of long sequences, 32 units, would go 79 -> 134)
   g.spread = !p.few && a.causal && g.units >= 64 * kXcds;
   const int64_t lines = g.by_xcd ? (g.units + kXcds - 1) / kXcds * kXcds : g.units;
   const dim3 grid((unsigned)(lines * p.tiles * p.nsplit)), block(p.waves * 64);
