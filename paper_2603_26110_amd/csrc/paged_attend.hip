@@ -932,9 +932,11 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   g.units = (int)(p.units / p.tiles);
   g.tiles = p.tiles;
   g.by_xcd = g.units % kXcds == 0 || g.units >= 8 * kXcds;
-  // (64 ragged prompts of 20 heads, 1280 units: 223 -> 200 us; four chunks on top
-  // of long sequences, 32 units, would go 79 -> 134)
-  g.spread = !p.few && a.causal && g.units >= 64 * kXcds;
+  // Where blocks differ, by what their rows see or by their sequences' lengths, and
+  // there are units enough (64 ragged prompts of 20 heads, 1280 units: causal 223
+  // -> 200 us, else 352 -> 310; one sequence of 660 units, not causal, would go 344
+  // -> 356; four chunks on top of long sequences, 32 units, 79 -> 134).
+  g.spread = !p.few && (a.causal || a.B > 1) && g.units >= 64 * kXcds;
   const int64_t lines = g.by_xcd ? (g.units + kXcds - 1) / kXcds * kXcds : g.units;
   const dim3 grid((unsigned)(lines * p.tiles * p.nsplit)), block(p.waves * 64);
   if (!p.few && p.groups == 1)

@@ -712,3 +712,10 @@ def test_two_streams_and_one_workspace_for_all_shapes():
     torch.cuda.synchronize()
     for g, x in zip(got, want):
         assert all(torch.equal(y, x) for y in g)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows_of_many_units(causal):               # 540 units, of two row tiles and of none
+    w = World([140, 0, 33, 70, 200, 64, 129, 80, 66], [130, 0, 33, 2, 66, 64, 129, 10, 65], 20, 20, layers=3, seed=9)
+    got = w.call(causal)
+    w.check(got, causal)
