@@ -600,7 +600,11 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
 // GROUPS: 1: one group of four waves, 128 rows a block. 2: two groups of two
 // waves, 64 rows a block, that take every other page each and are joined at the
 // end: twice the blocks and half the pages one after the other, for calls that
-// do not fill the chip.
+// do not fill the chip. Two groups have one buffer each and a second barrier, so
+// that three blocks fit a compute unit, not two (16-bit results: four chunks 82 ->
+// 74 us, 20 heads of 8 ragged sequences of up to 500 tokens 37 -> 32, one prompt of
+// 1024 20.5 -> 20.9); with fp32 results they keep two (38 us against 42 for two
+// sequences of 1000).
 //
 // Values are converted over the reference scale of the output's sums, times the
 // power of two by which the page's scale differs (fp16 holds 448 * 2^6 and the
@@ -611,8 +615,10 @@ constexpr int kFrag = 64 * 16;                        // bytes of an operand of 
 template <int IO, int PREC, int ROPE, int GROUPS>
 __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid grid) {
   constexpr int kWaves = 4 / GROUPS, kThreads = 64 * kWaves;   // of a group
+  constexpr int kBuffers = GROUPS == 2 && PREC < 2 ? 1 : 2;
+  static_assert(2 * 34 * 64 * 4 <= 32 * kFrag && 2 * kRowsMany * kMaxSplit * 8 <= 32 * kFrag, "room for the groups' sums, and the splits'");
   // [group][buffer][keys: 32-token half T, step | values: 32-dimension half, step][lane]
-  __shared__ __align__(16) uint8_t s_page[GROUPS][2][16 * kFrag];
+  __shared__ __align__(16) uint8_t s_page[GROUPS * kBuffers * 16 * kFrag];
   __shared__ int s_most[4];
   const Place place = place_of(a, grid);
   if (!place.there) return;
@@ -756,10 +762,11 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
   const uint32_t kfrom[2] = {(uint32_t)(32 * half + (c32 ^ (8 * half))) * 16, (uint32_t)(32 * half + (c32 ^ (4 + 8 * half))) * 16};
   auto frag = [&](const uint8_t* from, int i, uint32_t at) { return *reinterpret_cast<const f16x8*>(from + i * kFrag + at); };
 
-  if (begin < ntiles) stage(s_page[group][0], begin);
+  auto page_of = [&](int buffer) { return s_page + (group * kBuffers + buffer) * 16 * kFrag; };
+  if (begin < ntiles) stage(page_of(0), begin);
   int buffer = 0;
-  for (int tl = begin; tl < ntiles + group; tl += GROUPS, buffer ^= 1) {   // (the same turns for all groups)
-    const uint8_t* from = s_page[group][buffer];
+  for (int tl = begin; tl < ntiles + group; tl += GROUPS, buffer = (buffer + 1) % kBuffers) {   // (the same turns for all groups)
+    const uint8_t* from = page_of(buffer);
     const float kscale = sc.x, move = moved, over = vscale;
     const bool more = tl + GROUPS < ntiles;
     if (more) {
@@ -835,7 +842,8 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
           O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[u], O[d], 0, 0, 0);
         }
     }
-    if (more) stage(s_page[group][buffer ^ 1], tl + GROUPS);
+    if (kBuffers == 1) __syncthreads();
+    if (more) stage(page_of((buffer + 1) % kBuffers), tl + GROUPS);
   }
   lsum += __shfl_xor(lsum, 32, 64);
   if constexpr (GROUPS == 2) {
@@ -892,7 +900,7 @@ AttendPlan plan_attend(int64_t units0, int64_t rows, int max_len) {
   p.few = rows <= 64;
   // Blocks of 128 rows where these fill the chip three times, else of 64 (an
   // encoder's 5280 blocks of 128 rows 346 us against 439; 640 blocks of four
-  // chunks 91 against 79, 160 of one prompt 27 against 20).
+  // chunks 91 against 75, 160 of one prompt 27 against 21).
   p.groups = units0 * ((rows + 4 * kRowsMany - 1) / (4 * kRowsMany)) < 768 ? 2 : 1;
   const int per = p.few ? kRowsFew : 4 * kRowsMany / p.groups;
   p.tiles = (int)((rows + per - 1) / per);
@@ -935,7 +943,7 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   // Where blocks differ, by what their rows see or by their sequences' lengths, and
   // there are units enough (64 ragged prompts of 20 heads, 1280 units: causal 223
   // -> 200 us, else 352 -> 310; one sequence of 660 units, not causal, would go 344
-  // -> 356; four chunks on top of long sequences, 32 units, 79 -> 134).
+  // -> 356; four chunks on top of long sequences, 32 units, with two buffers 79 -> 134).
   g.spread = !p.few && (a.causal || a.B > 1) && g.units >= 64 * kXcds;
   const int64_t lines = g.by_xcd ? (g.units + kXcds - 1) / kXcds * kXcds : g.units;
   const dim3 grid((unsigned)(lines * p.tiles * p.nsplit)), block(p.waves * 64);
