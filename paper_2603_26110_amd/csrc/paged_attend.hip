@@ -366,7 +366,7 @@ template <int IO, int PREC, int ROPE, int W>
 __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendArgs a, AttendGrid grid) {
   constexpr int kStride = kDim + 4;
   __shared__ float s_m[W][kRowsFew], s_l[W][kRowsFew];
-  static_assert(W * kStride >= 2 * kMaxSplit, "room for the splits' statistics");
+  static_assert(W == 1 || W * kStride >= 2 * kMaxSplit, "room for the splits' statistics");   // (one wave: no splits)
   __shared__ __align__(16) float s_o[W * kRowsFew * kStride];
   __shared__ int s_last;
   const Place place = place_of(a, grid);
@@ -922,6 +922,11 @@ AttendPlan plan_attend(int64_t units0, int64_t rows, int max_len) {
   // units of 128 pages 128 -> 126 us); four else (660 units of 17 pages 22.7
   // against 27.3 us: more blocks fit a compute unit at once).
   if ((p.units <= 256 && pages >= 16) || pages >= 64) p.waves = 8;
+  // One wave where many units have few pages for it: a block's start and end cost as
+  // much as several pages (21 120 units of two pages 164 -> 74 us, of four 191 -> 127,
+  // of eight 273 -> 243, of twelve 360 -> 350; 2400 units of two 22 -> 13, of eight
+  // 36 -> 32).
+  if (pages <= 8 && p.units >= 2048) p.waves = 1;
   // A unit's pages are shared by blocks, with two pages a wave, where the blocks
   // find free compute units and each wave is spared two and a half pages, at
   // about 1.1 us each: storing and joining costs 2.5 us and more (20 units of
@@ -951,6 +956,8 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
     hipLaunchKernelGGL((attend_many<IO, PREC, ROPE, 1>), grid, block, 0, st, a, g);
   else if (!p.few)
     hipLaunchKernelGGL((attend_many<IO, PREC, ROPE, 2>), grid, block, 0, st, a, g);
+  else if (p.waves == 1)
+    hipLaunchKernelGGL((attend_few<IO, PREC, ROPE, 1>), grid, block, 0, st, a, g);
   else if (p.waves == 8)
     hipLaunchKernelGGL((attend_few<IO, PREC, ROPE, 8>), grid, block, 0, st, a, g);
   else

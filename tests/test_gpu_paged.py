@@ -719,3 +719,16 @@ def test_many_rows_of_many_units(causal):               # 540 units, of two row 
     w = World([140, 0, 33, 70, 200, 64, 129, 80, 66], [130, 0, 33, 2, 66, 64, 129, 10, 65], 20, 20, layers=3, seed=9)
     got = w.call(causal)
     w.check(got, causal)
+
+
+@pytest.mark.parametrize("dtype,rope,out_f32", [(F16, "pairs", False), (BF16, "half", True), (F32, "none", False)])
+def test_many_short_sequences(dtype, rope, out_f32):    # 4160 units of up to four pages
+    lens = [0, 1, 63, 64, 65, 128, 129, 192, 200, 255, 256] + list(range(2, 23)) + [70, 130] * 10
+    w = World(lens, [1 if n else 0 for n in lens], 40, 20, dtype=dtype, rope=rope, layers=4, seed=11, out_f32=out_f32)
+    w.check(w.call())
+    w.check(w.call(False), False)
+    table = [row[:] for row in w.table]
+    table[5][1] = w.pages                               # a page that is not there
+    again = w.call(table=i32(table))
+    assert bool(again[:, w.row0[5]].isnan().all()) and not bool(again[:, :w.row0[5]].isnan().any())
+    assert not bool(again[:, w.row0[6]:].isnan().any())
