@@ -181,7 +181,7 @@ TQ_API tq_status tqp_append(const tqp_params* params, const tqp_cache* cache, co
  *   max_new, max_len  host bounds on the rows and tokens of a sequence. A call
  *           whose nlayers * B * kv_heads times the row tiles of max_new (64 or
  *           128 rows; 16 where max_new * num_heads / kv_heads <= 64) would
- *           need 2^32 threads is refused.
+ *           need 2^32 threads (256 or 512 a tile) is refused.
  *   out     device [nlayers][rows][num_heads][64] of io_dtype, or fp32 with
  *           TQ_OUT_FP32, contiguous, 16-byte aligned.
  *   workspace device, >= tqp_workspace_bytes(...) bytes, 16-byte aligned (NULL

@@ -197,8 +197,9 @@ tq_status tqp_attend(const tqp_params* params, const tqp_cache* cache, const tqp
   if (too_many_units(nlayers, B, params->kv_heads, unit_rows) || (int64_t)rows * group >= ((int64_t)1 << 30))
     return fail(TQ_ERR_ARG, "too many rows or units for one call");
   const tqp::AttendPlan plan = tqp::plan_attend((int64_t)nlayers * B * params->kv_heads, unit_rows, max_len);
-  // (a launch has fewer than 2^32 threads; the grid is padded by up to seven units)
-  if ((plan.units + 8 * (int64_t)plan.tiles) * plan.nsplit >= ((int64_t)1 << 32) / (64 * plan.waves))
+  // (a launch has fewer than 2^32 threads; the grid is padded by up to seven units;
+  // blocks of one wave count as four, so that the limit does not grow for short max_len)
+  if ((plan.units + 8 * (int64_t)plan.tiles) * plan.nsplit >= ((int64_t)1 << 32) / (64 * std::max(plan.waves, 4)))
     return fail(TQ_ERR_ARG, "too many rows or units for one call");
   if (plan.workspace > 0) {
     if (!workspace) return fail(TQ_ERR_CAPACITY, "workspace of %zu bytes required", plan.workspace);
