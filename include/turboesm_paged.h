@@ -170,7 +170,9 @@ TQ_API tq_status tqp_append(const tqp_params* params, const tqp_cache* cache, co
  *   NaN: the rows of a sequence whose length is negative, above max_len or
  *   above 64*table_width or which has more than max_new rows; a row with
  *   pos < 0, or (with rope_cs) pos >= rope_positions; a row that sees a token
- *   whose table entry is outside [0, pages). Rows that no sequence has
+ *   whose table entry is outside [0, pages); a row whose q' is not finite, or
+ *   whose scores all lie below binary32's range or one above it, and that sees
+ *   a token. Rows that no sequence has
  *   (before row0[0], from row0[B] on) are not written. row0 must not decrease
  *   and must lie within [0, rows]: a sequence whose rows do not is skipped.
  *

@@ -295,11 +295,12 @@ __device__ __forceinline__ uint32_t below(int first, int len) {
   return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
 }
 
-// Four dimensions of a row's result, o / l.
+// Four dimensions of a row's result, o / l. A row that sees tokens and has no
+// weight has -infinity for all its scores (of an infinite query, say): 0 / 0.
 template <int IO>
 __device__ __forceinline__ void store_result(const AttendArgs& a, const Sequence& s, int l, int h, int f, int d, f32x4 o, float sum) {
   const Row x = row_of(a, s, h, f);
-  const float by = !x.fine ? __builtin_nanf("") : sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float by = !x.fine ? __builtin_nanf("") : x.sees <= 0 ? 0.0f : 1.0f / sum;
   store_four<IO>(a, (((int64_t)l * a.rows + x.row) * a.heads + x.head) * kDim + d, o[0] * by, o[1] * by, o[2] * by, o[3] * by);
 }
 
@@ -884,7 +885,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
     }
   }
   if (!r.there) return;
-  const float f = !r.fine ? __builtin_nanf("") : lsum == 0.0f ? 0.0f : scale / lsum;
+  const float f = !r.fine ? __builtin_nanf("") : r.sees <= 0 ? 0.0f : scale / lsum;   // (as in store_result)
   const int64_t at = (((int64_t)l * a.rows + r.row) * a.heads + r.head) * kDim + 4 * half;
 #pragma unroll
   for (int d = 0; d < 2; ++d)

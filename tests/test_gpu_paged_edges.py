@@ -1,0 +1,41 @@
+"""The paged cache at the edges of what it documents: queries and scores past the ordinary, value scales far apart, bad
+pages, the types and pairings that the other tests do not reach."""
+
+import pytest
+import torch
+
+from test_gpu_paged import BF16, DEV, F16, F32, World, i32
+
+pytestmark = pytest.mark.gpu
+
+# (lens, new, heads, kv_heads): every kind of launch that attention has
+FEW = {"four_waves": ([200, 65], [1, 2], 6, 2), "eight_waves": ([1025], [1], 4, 4), "splits": ([8192], [1], 4, 1),
+       "one_wave": ([130] * 64, [1] * 64, 32, 32)}
+MANY = {"two_groups": ([200, 90], [70, 66], 2, 1), "splits": ([9000], [70], 2, 1), "one_group": ([130] * 32, [129] * 32, 12, 12)}
+ALL = {**{"few_" + k: v for k, v in FEW.items()}, **{"many_" + k: v for k, v in MANY.items()}}
+
+
+# ---------------------------------------------------------------- queries
+@pytest.mark.parametrize("dtype,rope,out_f32", [(BF16, "none", False), (F16, "none", False), (BF16, "half", False),
+                                                (F16, "pairs", False), (F32, "none", False), (F16, "none", True)])
+@pytest.mark.parametrize("kind", list(ALL))
+def test_an_infinite_query_has_no_result(kind, dtype, rope, out_f32):
+    # every key has one sign in the query's infinite channel, so that every score is -inf: the mask's value
+    w = World(*ALL[kind], dtype=dtype, rope=rope, out_f32=out_f32, seed=31)
+    k, _, _ = w.cache.values()
+    codes = w.cache.k_codes.view(w.params.num_layers, w.params.kv_heads, w.pages, 64, 64)
+    codes[..., 3] |= 0x80                                  # (negative; no code of this world's is NaN)
+    codes[..., 3] = torch.where(codes[..., 3] == 0x80, 0x90, codes[..., 3].int()).to(torch.uint8)
+    fine = w.call()
+    w.check(fine)
+    q = w.q.clone()
+    rows = sorted({0, w.rows // 2, w.rows - 1})
+    q[:, rows, :, 3] = float("inf")
+    for causal in (True, False):
+        got, other = w.call(causal, q=q), w.call(causal)
+        assert bool(got[:, rows].isnan().all())
+        rest = torch.ones(w.rows, dtype=torch.bool, device=DEV)
+        rest[rows] = False
+        assert torch.equal(got[:, rest], other[:, rest])
+    empty = w.call(q=q, seq_len=i32([0] * len(w.lens)))   # (a row that sees nothing has no score either)
+    assert bool((empty == 0).all())
