@@ -117,15 +117,17 @@ __global__ __launch_bounds__(kThreads) void assign_kernel(AssignArgs a) {
   if (taken) atomicMax(&s_taken, taken);
   __syncthreads();
   if (blockIdx.x == 0 && t == 0) a.row0[B] = s_row0[B];
-  const int end = s_row0[B];
-  for (int row = blockIdx.x * kThreads + t; row < a.rows; row += gridDim.x * kThreads) {
+  // (rows are counted without a sign: the step past the last of 2^31 - 1 stays below 2^32)
+  const uint32_t rows = (uint32_t)a.rows, end = (uint32_t)s_row0[B];
+  static_assert((uint64_t)INT32_MAX + (uint64_t)kMost * kThreads <= UINT32_MAX, "a row number wraps");
+  for (uint32_t row = blockIdx.x * kThreads + t; row < rows; row += gridDim.x * kThreads) {
     int64_t slot = -1;
     int pos = -1;
     if (row < end) {
-      const int b = owner_of(s_row0, B, row);
+      const int b = owner_of(s_row0, B, (int)row);
       if (s_take[b] >= 0) {
         const int len = s_len[b], held = pages_of(len);
-        pos = len + row - s_row0[b];
+        pos = len + ((int)row - s_row0[b]);
         const int p = pos / kPage;
         int32_t* entry = a.pool.table + (int64_t)b * a.pool.width + p;
         int page;

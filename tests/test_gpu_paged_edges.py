@@ -4,6 +4,7 @@ pages, the types and pairings that the other tests do not reach."""
 import pytest
 import torch
 
+from paper_2603_26110_amd import paged
 from test_gpu_paged import BF16, DEV, F16, F32, World, i32
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,20 @@ def test_an_infinite_query_has_no_result(kind, dtype, rope, out_f32):
         assert torch.equal(got[:, rest], other[:, rest])
     empty = w.call(q=q, seq_len=i32([0] * len(w.lens)))   # (a row that sees nothing has no score either)
     assert bool((empty == 0).all())
+
+
+# ------------------------------------------------------------------ pages
+def test_assign_of_as_many_rows_as_there_are_numbers():
+    # 2^31 - 1 rows, all but 75 of them padding: a row number past the last does not come back as a negative one
+    rows, before = 2 ** 31 - 1, 1 << 17
+    slots = torch.full((before + rows,), 7, dtype=torch.int64, device=DEV)
+    pos = torch.full((before + rows,), 7, dtype=torch.int32, device=DEV)
+    pool, table, lens = paged.PagePool(8), torch.full((2, 2), -1, dtype=torch.int32, device=DEV), i32([0, 0])
+    paged.assign(pool, table, lens, i32([5, 70]), rows, out=(slots[before:], pos[before:], i32([0] * 3), i32([0] * 2)))
+    assert lens.tolist() == [5, 70] and table.tolist() == [[0, -1], [1, 2]] and pool.state.tolist() == [5, 0, 0, 0]
+    want = list(range(5)) + list(range(64, 134))
+    assert slots[before:before + 75].tolist() == want and pos[before:before + 75].tolist() == list(range(5)) + list(range(70))
+    for t in (slots, pos):
+        assert bool((t[:before] == 7).all())
+        for i in range(before + 75, before + rows, 1 << 28):
+            assert bool((t[i:i + (1 << 28)] == -1).all())
