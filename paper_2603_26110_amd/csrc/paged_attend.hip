@@ -289,6 +289,23 @@ __device__ __forceinline__ float score_scale(float row, float page) {
   return __builtin_amdgcn_fmed3f(row * page, 1e-37f, 3e38f);
 }
 
+// Sums O are in units of a page's value scale, and a page's values are at most
+// 448 * 2^47: with weights of W in all, |O| <= 2^56 W / scale. W is below 2^45
+// (2^30 tokens of 2^15), so that O stays within binary32 for scales from 2^-24
+// on. Before O moves to a smaller one the reference of the exponents rises until
+// the weights (of which `some` is a quarter at least) sum to 2^18 at most, and
+// then |O| <= 2^122. (Of n tokens the largest weight is still 2^15 / n or more.)
+constexpr float kSmallScale = 0x1p-24f;
+template <class T, int N>
+__device__ __forceinline__ void ease(float some, float& m, float& lsum, T (&O)[N]) {
+  const float next = m + (float)max(((__float_as_int(some) >> 23) & 0xFF) - 127 - 15, 0);
+  const float f = __builtin_amdgcn_exp2f(m - next);
+  m = next;
+  lsum *= f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) O[i] *= f;
+}
+
 // Bytes of the tokens first .. first+3 that are below len.
 __device__ __forceinline__ uint32_t below(int first, int len) {
   const int n = len - first;
@@ -466,6 +483,7 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
   }
 
   auto attend = [&](int tl, int next, bool next_bad) {   // next: the page after this one, or -1
+    if (sc.y != vscale && sc.y < kSmallScale) ease(max_across16(max_across32(lsum)), m, lsum, O);   // (uniform)
     f32x4 S[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -613,8 +631,10 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
 // differs by more.
 constexpr int kFrag = 64 * 16;                        // bytes of an operand of one instruction
 
+// Four waves a SIMD where nothing is in two parts (129 registers without the bound: an
+// encoder's bf16 results 287 us, 262 with it).
 template <int IO, int PREC, int ROPE, int GROUPS>
-__global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid grid) {
+__global__ __launch_bounds__(256, PREC == 0 && GROUPS == 1 ? 4 : 2) void attend_many(AttendArgs a, AttendGrid grid) {
   constexpr int kWaves = 4 / GROUPS, kThreads = 64 * kWaves;   // of a group
   constexpr int kBuffers = GROUPS == 2 && PREC < 2 ? 1 : 2;
   static_assert(2 * 34 * 64 * 4 <= 32 * kFrag && 2 * kRowsMany * kMaxSplit * 8 <= 32 * kFrag, "room for the groups' sums, and the splits'");
@@ -778,6 +798,7 @@ __global__ __launch_bounds__(256, 2) void attend_many(AttendArgs a, AttendGrid g
     const bool works = tl < min(mine, ntiles);
     f16x8 ph[4], pl[4];
     if (works) {
+      if (move != 1.0f && over < kSmallScale) ease(max_across32(lsum), m, lsum, O);   // (uniform)
       f32x16 S[2];
 #pragma unroll
       for (int T = 0; T < 2; ++T) {

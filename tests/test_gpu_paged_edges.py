@@ -1,6 +1,8 @@
 """The paged cache at the edges of what it documents: queries and scores past the ordinary, value scales far apart, bad
 pages, the types and pairings that the other tests do not reach."""
 
+import math
+
 import pytest
 import torch
 
@@ -40,6 +42,37 @@ def test_an_infinite_query_has_no_result(kind, dtype, rope, out_f32):
         assert torch.equal(got[:, rest], other[:, rest])
     empty = w.call(q=q, seq_len=i32([0] * len(w.lens)))   # (a row that sees nothing has no score either)
     assert bool((empty == 0).all())
+
+
+# ----------------------------------------------------------- value scales
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,new", [(160, 1), (165, 65), (770, 65)])
+def test_value_scales_far_apart_after_many_tokens(B, new, dtype):
+    """A first page with scores of zero, pages whose scores are 2^14.9 times the weight and whose values are the largest
+    that there are, then pages of the smallest scale. Every sequence owns the same pages, and its rows see all."""
+    n, low, high = 160, 16, 128                           # pages: scores of zero; high scores and values; the rest small
+    cache, params = paged.Cache(1, 1, n), paged.Params(1, 1, 1, None, dtype, softmax_scale=math.log(2.0))
+    k, v, s = cache.values()
+    k.zero_()
+    v[:] = torch.ones_like(v)
+    k[:, :, low:low + high, :, 0] = torch.full((1, 1, high, 64), 15.0, device=DEV).to(k.dtype)   # (the score's log2)
+    k[:, :, low + high:, :, 0] = torch.full((1, 1, n - low - high, 64), -1.0, device=DEV).to(k.dtype)
+    v[:, :, low:low + high] = torch.full((1, 1, high, 4, 4, 4, 64), 448.0, device=DEV).to(v.dtype)
+    s[..., 0] = 1.0
+    s[..., 1] = 2.0 ** -48
+    s[:, :, low:low + high, 1] = 2.0 ** 47
+    rows = B * new
+    q = torch.zeros((1, rows, 1, 64), device=DEV, dtype=dtype)
+    q[..., 0] = 0.5                                       # (15 / 2 above the first page: the reference does not move)
+    row0 = i32(list(range(0, rows + 1, new)))
+    got = paged.attend(params, cache, q, i32([64 * n - 1] * rows), row0, i32([list(range(n))] * B), i32([64 * n] * B), new,
+                       64 * n, causal=False)
+    weight = 2.0 ** torch.tensor([0.0] * low + [7.5] * high + [-0.5] * (n - low - high), dtype=torch.float64)
+    value = torch.tensor([2.0 ** -48] * low + [448.0 * 2.0 ** 47] * high + [2.0 ** -48] * (n - low - high), dtype=torch.float64)
+    want = float((weight * value).sum() / weight.sum())
+    # weights to 2^-11 (fp16) each above and below, sums of 10240 terms in binary32, the result's own rounding
+    tol = (2 * 2.0 ** -11 + 2 * 10304 * 2.0 ** -24 + torch.finfo(got.dtype).eps / 2) * abs(want)
+    assert float((got.double() - want).abs().max()) <= tol
 
 
 # ------------------------------------------------------------------ pages
