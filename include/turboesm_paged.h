@@ -34,6 +34,10 @@
  *   scales: fp32 [L][kv_heads][pages][2], the page's key and value scale.
  *   A value is its code's e4m3 value (OCP e4m3fn) times its scale. Scales
  *   are powers of two 2^E with E in [-48, 47].
+ * Memory that tqp_append has not written may hold anything, but for the tokens
+ * below a seq_len that tqp_attend is given: each has to be one that tqp_append
+ * wrote, or its page has to be one whose value codes are no NaN (0x7F, 0xFF)
+ * and whose scales are as above. (Zeros and 2^-48, say.)
  */
 #ifndef TURBOESM_PAGED_H
 #define TURBOESM_PAGED_H

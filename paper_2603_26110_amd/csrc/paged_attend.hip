@@ -432,8 +432,10 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
 
   // One page: its keys (row c16 of the 16 tokens of part j, bytes 16 g .. +15)
   // and values (dimension 16 j + c16, the sixteen tokens of group g).
+  // One that is not there is page 0 with keys of NaN, values of zero and the scale
+  // of the page before, so that only rows that see it get NaN, whatever page 0 holds.
   u32x4 kw[4], vw[4];
-  float2 sc;
+  float2 sc = make_float2(1.0f, 1.0f);
   auto page_of = [&](int i, bool& bad) {
     const int page = __builtin_amdgcn_readlane(entries, i);
     bad = page < 0 || page >= a.cache.pages;
@@ -443,22 +445,28 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
     const uint8_t* p = kplane + (int64_t)page * kPageBytes;
 #pragma unroll
     for (int j = 0; j < 4; ++j) kw[j] = *reinterpret_cast<const u32x4*>(p + koff + j * 1024);
+    const float before = sc.y;
     sc = scales[page];
     if (bad) {
+      sc = make_float2(1.0f, before);
 #pragma unroll
       for (int j = 0; j < 4; ++j) kw[j] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
     }
   };
-  auto load_values = [&](int page) {
+  auto load_values = [&](int page, bool bad) {
     const uint8_t* p = vplane + (int64_t)page * kPageBytes;
 #pragma unroll
     for (int j = 0; j < 4; ++j) vw[j] = *reinterpret_cast<const u32x4*>(p + voff + j * 256);
+    if (bad) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vw[j] = u32x4{};
+    }
   };
   // The wave's first keys, before the query is worked on (with the values, too,
   // registers would spill).
+  bool bad = false;
   auto start = [&](int first) {
     if (a.nsplit > 1 || first > begin) entries = lane < (end - first + W - 1) / W ? table[first + lane * W] : 0;
-    bool bad;
     const int page = page_of(0, bad);
     load_keys(page, bad);
     return page;
@@ -555,14 +563,14 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
       O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, ph[0], O[d], 0, 0, 0);
       O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, ph[1], O[d], 0, 0, 0);
     }
-    if (next >= 0) load_values(next);
+    if (next >= 0) load_values(next, next_bad);
   };
   for (int first = begin; first < end; first += 64 * W) {
     const int n = min(64, (end - first + W - 1) / W);
     if (first > begin) page = start(first);
-    load_values(page);
+    load_values(page, bad);
     for (int i = 0; i < n; ++i) {
-      bool bad = false;
+      bad = false;
       page = i + 1 < n ? page_of(i + 1, bad) : -1;
       attend(first + i * W, page, bad);
     }
@@ -703,9 +711,13 @@ __global__ __launch_bounds__(256, PREC == 0 && GROUPS == 1 ? 4 : 2) void attend_
       vw[i] = vp[i * kThreads];
     }
     next_sc = scales[page];
-    if (bad) {
+    if (bad) {                   // (as for few rows)
+      next_sc = make_float2(1.0f, sc.y);
 #pragma unroll
-      for (int i = 0; i < GROUPS; ++i) kw[i] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+      for (int i = 0; i < GROUPS; ++i) {
+        kw[i] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+        vw[i] = u32x4{};
+      }
     }
   };
   // Key operands: step i, lane (half, token): dimensions 32 half + 8 i .. +7.

@@ -75,6 +75,37 @@ def test_value_scales_far_apart_after_many_tokens(B, new, dtype):
     assert float((got.double() - want).abs().max()) <= tol
 
 
+# -------------------------------------------------------------- bad pages
+ENDS = {"few_four_waves": ([66, 130], [4, 4], 6, 2), "few_eight_waves": ([64 * 17 + 2], [4], 4, 4),
+        "few_splits": ([8194], [4], 4, 1), "few_one_wave": ([66, 130] * 32, [4] * 64, 32, 32),
+        "many_two_groups": ([130, 66], [70, 66], 2, 1), "many_splits": ([9002], [70], 2, 1),
+        "many_one_group": ([130] * 32, [129] * 32, 12, 12)}
+
+
+@pytest.mark.parametrize("dtype,rope", [(BF16, "none"), (F32, "pairs")])
+@pytest.mark.parametrize("kind", list(ENDS))
+def test_a_bad_page_touches_only_the_rows_that_see_it(kind, dtype, rope):
+    """The last page of every sequence is not there, and page 0, which no sequence has, holds no numbers at all."""
+    w = World(*ENDS[kind], dtype=dtype, rope=rope, seed=32)
+    c, spare = w.cache, next(p for p in range(1, w.pages) if all(p not in row for row in w.table))
+    for t in (c.k_codes, c.v_codes, c.scales):
+        t[:, :, spare] = t[:, :, 0]
+    w.table = [[spare if p == 0 else p for p in row] for row in w.table]
+    fine = w.call()
+    w.check(fine)
+    table, sees = [list(row) for row in w.table], torch.zeros(w.rows, dtype=torch.bool, device=DEV)
+    for b, n in enumerate(w.lens):
+        last = (n - 1) // 64
+        table[b][last] = (-1, w.pages, 2 ** 31 - 1)[b % 3]
+        for t in range(w.row0[b], w.row0[b + 1]):
+            sees[t] = w.pos[t] >= 64 * last
+    assert bool(sees.any()) and not bool(sees.all())
+    for codes, scales in ((0x7F, 0.0), (0xFF, float("nan")), (0x7F, float("inf"))):
+        c.k_codes[:, :, 0], c.v_codes[:, :, 0], c.scales[:, :, 0] = codes, codes, scales
+        got = w.call(table=i32(table))
+        assert bool(got[:, sees].isnan().all()) and torch.equal(got[:, ~sees], fine[:, ~sees])
+
+
 # ------------------------------------------------------------------ pages
 def test_assign_of_as_many_rows_as_there_are_numbers():
     # 2^31 - 1 rows, all but 75 of them padding: a row number past the last does not come back as a negative one
