@@ -262,10 +262,12 @@ __device__ __forceinline__ void rotate_query(const Query<IO, N, ROPE>& q, int d0
 }
 
 // The exponent of a row's largest entry (from its bits): a row over 2^e has
-// entries up to 2 in fp16, whatever the type's range. Rows of zeros, and what
-// is no number, stay as they are.
+// entries up to 2 in fp16, whatever the type's range, and steps of 2^-24 at
+// least. Rows of zeros, and what is no number, stay as they are, and so do fp16
+// entries that were not rotated: they are fp16 values.
+template <int IO, int ROPE>
 __device__ __forceinline__ int row_exponent(uint32_t amax) {
-  return amax < 0x00800000u || amax >= kInfBits ? 0 : (int)(amax >> 23) - 127;
+  return (IO == kF16 && ROPE == kNone) || amax < 0x00800000u || amax >= kInfBits ? 0 : (int)(amax >> 23) - 127;
 }
 
 // x 2^-e in two steps (e may be -126 .. 127).
@@ -484,7 +486,7 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
     for (int i = 0; i < 16; ++i) m = max(m, abs_bits(x[i]));
     m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
     m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
-    const int e = row_exponent(m);
+    const int e = row_exponent<IO, ROPE>(m);
     split8<PREC>(x, e, qh[0], ql[0]);
     split8<PREC>(x + 8, e, qh[1], ql[1]);
     rowscale = a.scale2 * pow2(max(e, -126));
@@ -784,7 +786,7 @@ __global__ __launch_bounds__(256, PREC == 0 && GROUPS == 1 ? 4 : 2) void attend_
 #pragma unroll
     for (int i = 0; i < 32; ++i) m = max(m, abs_bits(x[i]));
     m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
-    const int e = row_exponent(m);
+    const int e = row_exponent<IO, ROPE>(m);
 #pragma unroll
     for (int i = 0; i < 4; ++i) split8<PREC>(x + 8 * i, e, qh[i], ql[i]);
     rowscale = a.scale2 * pow2(max(e, -126));
@@ -1010,7 +1012,7 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   if (a.io == kF32) return launch<kF32, 2>(a, p, st);
   if (a.io == kF16 && a.out_f32) return launch<kF16, 2>(a, p, st);
-  // (an fp16 query that is not rotated is an fp16 value as it is)
+  // (an fp16 query that is not rotated is exact in one part)
   if (a.io == kF16) return a.cs ? launch<kF16, 1>(a, p, st) : launch<kF16, 0, kNone>(a, p, st);
   return a.out_f32 ? launch<kBF16, 2>(a, p, st) : launch<kBF16, 0>(a, p, st);
 }

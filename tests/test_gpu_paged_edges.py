@@ -44,6 +44,18 @@ def test_an_infinite_query_has_no_result(kind, dtype, rope, out_f32):
     assert bool((empty == 0).all())
 
 
+@pytest.mark.parametrize("out_f32", [False, True])
+@pytest.mark.parametrize("kind", list(ALL))
+def test_an_fp16_query_without_rope_is_exact(kind, out_f32):
+    # a channel of the largest size, in which the keys are zero, takes no bits from the others (down to fp16's lowest)
+    w = World(*ALL[kind], dtype=F16, rope="none", out_f32=out_f32, seed=33, scale=8.0)
+    w.cache.k_codes.view(w.params.num_layers, w.params.kv_heads, w.pages, 64, 64)[..., 7] = 0
+    w.q *= 2.0 ** -6
+    w.q[..., 20:40] *= 2.0 ** -9
+    w.q[..., 7] = 65504.0
+    w.check(w.call())
+
+
 # ----------------------------------------------------------- value scales
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,new", [(160, 1), (165, 65), (770, 65)])
