@@ -261,16 +261,17 @@ __device__ __forceinline__ void rotate_query(const Query<IO, N, ROPE>& q, int d0
   }
 }
 
-// The exponent of a row's largest entry (from its bits): a row over 2^e has
-// entries up to 2 in fp16, whatever the type's range, and steps of 2^-24 at
-// least. Rows of zeros, and what is no number, stay as they are, and so do fp16
+// The power of two that a row is divided by, from its largest entry's bits: 2^14
+// to 2^15 in fp16 then, so that fp16's lowest step is 2^-38 of it and a large
+// channel takes no bits from the others (64 products with codes of 448 are below
+// 2^30). Rows of zeros, and what is no number, stay as they are, and so do fp16
 // entries that were not rotated: they are fp16 values.
 template <int IO, int ROPE>
 __device__ __forceinline__ int row_exponent(uint32_t amax) {
-  return (IO == kF16 && ROPE == kNone) || amax < 0x00800000u || amax >= kInfBits ? 0 : (int)(amax >> 23) - 127;
+  return (IO == kF16 && ROPE == kNone) || amax < 0x00800000u || amax >= kInfBits ? 0 : (int)(amax >> 23) - 127 - 14;
 }
 
-// x 2^-e in two steps (e may be -126 .. 127).
+// x 2^-e in two steps (e may be -140 .. 113).
 __device__ __forceinline__ float over_pow2(float x, int e) {
   return x * pow2(-(e >> 1)) * pow2(-(e - (e >> 1)));
 }

@@ -56,6 +56,18 @@ def test_an_fp16_query_without_rope_is_exact(kind, out_f32):
     w.check(w.call())
 
 
+@pytest.mark.parametrize("dtype,rope,out_f32", [(F16, "pairs", False), (F16, "half", True), (BF16, "pairs", False),
+                                                (BF16, "half", True), (F32, "pairs", False), (F32, "none", False)])
+@pytest.mark.parametrize("kind", list(ALL))
+def test_a_large_channel_takes_no_bits_from_the_others(kind, dtype, rope, out_f32):
+    # (the keys are zero in it and in its partner; the other channels decide the scores)
+    w = World(*ALL[kind], dtype=dtype, rope=rope, out_f32=out_f32, seed=34, scale=8.0)
+    w.cache.k_codes.view(w.params.num_layers, w.params.kv_heads, w.pages, 64, 64)[..., [6, 7, 39]] = 0
+    w.q *= 2.0 ** -6
+    w.q[..., 7] = 65504.0
+    w.check(w.call())
+
+
 # ----------------------------------------------------------- value scales
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,new", [(160, 1), (165, 65), (770, 65)])
