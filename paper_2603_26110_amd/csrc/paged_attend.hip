@@ -181,7 +181,7 @@ __device__ __forceinline__ Row row_of(const AttendArgs& a, const Sequence& s, in
   r.head = h * a.group + (r.there ? f - tok * a.group : 0);
   r.pos = a.pos[r.row];
   r.fine = r.there && r.pos >= 0 && (!a.cs || r.pos < a.rope_positions);
-  r.sees = !r.fine ? 0 : a.causal ? min(s.len, r.pos + 1) : s.len;
+  r.sees = !r.fine ? 0 : a.causal ? min(s.len - 1, r.pos) + 1 : s.len;   // (pos + 1 may pass 32 bits)
   return r;
 }
 

@@ -68,6 +68,15 @@ def test_a_large_channel_takes_no_bits_from_the_others(kind, dtype, rope, out_f3
     w.check(w.call())
 
 
+@pytest.mark.parametrize("kind", list(ALL))
+def test_positions_past_the_sequence_see_all_of_it(kind):
+    # without RoPE any position that is not negative is one: the largest, too
+    w = World(*ALL[kind], rope="none", seed=35)
+    want = w.call(False)
+    for p in (max(w.lens) - 1, 2 ** 24, 2 ** 31 - 2, 2 ** 31 - 1):
+        assert torch.equal(w.call(True, pos=i32([p] * w.rows)), want), p
+
+
 # ----------------------------------------------------------- value scales
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,new", [(160, 1), (165, 65), (770, 65)])
