@@ -39,7 +39,9 @@ constexpr int kPartRow = kDim + 4;                    // o[64], m, l of a row of
 // The largest weight is kept between 2^7 and 2^15: the reference of the exponents
 // is 7 below the running maximum and moves when a score is 15 above it. So
 // rescaling is rare, and the steps that fp16 has at its lower end, 2^-24, are
-// 2^-31 of the largest weight.
+// 2^-31 of the largest weight. (What a score is above the reference is looked at as a
+// difference: a sum with 15 rounds up where binary32 counts in eights, and 2^16 is
+// no fp16 value.)
 constexpr float kTop = 7.0f, kRaise = 15.0f;
 
 __device__ __forceinline__ float lowest() { return -3.40282347e38f; }
@@ -532,8 +534,8 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
 #pragma unroll
       for (int j = 0; j < 4; ++j) top = fmaxf(top, S[i][j]);
     top = max_across16(max_across32(top));
-    if (__any(top > m + kRaise)) {
-      const float next = top > m + kRaise ? top - kTop : m;
+    if (__any(top - m > kRaise)) {
+      const float next = top - m > kRaise ? top - kTop : m;
       const float f = __builtin_amdgcn_exp2f(m - next);
       m = next;
       lsum *= f;
@@ -826,7 +828,7 @@ __global__ __launch_bounds__(256, PREC == 0 && GROUPS == 1 ? 4 : 2) void attend_
         }
         S[T] = z;
       }
-      const float c = score_scale(rowscale, kscale);
+      float c = score_scale(rowscale, kscale);
       if ((tl + 1) * kPage > least) {
 #pragma unroll
         for (int T = 0; T < 2; ++T)
@@ -840,8 +842,16 @@ __global__ __launch_bounds__(256, PREC == 0 && GROUPS == 1 ? 4 : 2) void attend_
 #pragma unroll
         for (int j = 0; j < 16; j += 2) top = largest(largest(top, S[T][j]), S[T][j + 1]);
       top = max_across32(top) * c;
-      if (__any(top > m + kRaise)) {
-        const float next = top > m + kRaise ? top - kTop : m;
+      // The multiply-add below does not round a score, but top is rounded: from 2^25 on
+      // the two differ by powers of two, and a weight would leave fp16's range. So
+      // large scores are rounded before it.
+      if (__any(fabsf(top) > 0x1p20f && fabsf(top) < INFINITY)) {
+        S[0] *= c;
+        S[1] *= c;
+        c = 1.0f;
+      }
+      if (__any(top - m > kRaise)) {
+        const float next = top - m > kRaise ? top - kTop : m;
         const float f = __builtin_amdgcn_exp2f(m - next);
         m = next;
         lsum *= f;

@@ -6,6 +6,7 @@ import math
 import pytest
 import torch
 
+import paged_ref as ref
 from paper_2603_26110_amd import paged
 from test_gpu_paged import BF16, DEV, F16, F32, World, i32
 
@@ -75,6 +76,59 @@ def test_positions_past_the_sequence_see_all_of_it(kind):
     want = w.call(False)
     for p in (max(w.lens) - 1, 2 ** 24, 2 ** 31 - 2, 2 ** 31 - 1):
         assert torch.equal(w.call(True, pos=i32([p] * w.rows)), want), p
+
+
+@pytest.mark.parametrize("dtype,out_f32", [(F16, False), (BF16, False), (F32, False), (F16, True)])
+@pytest.mark.parametrize("kind", list(ALL))
+def test_scores_of_billions(kind, dtype, out_f32):
+    """Scores whose binary32 steps are larger than the range of the weights: the largest takes all."""
+    w = World(*ALL[kind], dtype=dtype, rope="none", out_f32=out_f32, seed=36, scale=1.0)
+    w.q *= 15000.0
+    w.cache.scales[..., 0] *= 2.0 ** 13
+    k, v, s = w.cache.values()
+    k = k.double() * s[..., 0].double()[..., None, None]
+    v = v.reshape(k.shape).double() * s[..., 1].double()[..., None, None]
+    got, G, clear, rows = w.call(False), w.params.num_heads // w.params.kv_heads, 0, 0
+    number = torch.isfinite(w.q).all(-1)                 # (15000 times a normal number may pass 65504)
+    assert torch.equal(torch.isfinite(got).all(-1), number) and torch.equal(got.isnan().any(-1), ~number)
+    half = torch.finfo(got.dtype).eps / 2
+    for b, n in enumerate(w.lens[:3]):
+        ids, lo, hi = w.table[b][:ref.pages_of(n)], w.row0[b], w.row0[b + 1]
+        kb, vb = (x[0][:, ids].reshape(w.params.kv_heads, -1, 64)[:, :n] for x in (k, v))
+        for h in range(w.params.num_heads):
+            q = w.q[0, lo:hi, h].double()
+            score, size = q @ kb[h // G].T, q.abs() @ kb[h // G].abs().T
+            two = score.topk(2, -1)
+            # the sum of 64 products rounds 64 times at most, its scaling and the difference three times
+            far = (two.values[:, 0] - two.values[:, 1] > 2 * 70 * 2.0 ** -24 * size.amax(-1) + 40) & number[0, lo:hi, h]
+            clear, rows = clear + int(far.sum()), rows + hi - lo
+            want = vb[h // G][two.indices[:, 0]]
+            off = (got[0, lo:hi, h].double() - want).abs()[far]
+            # (the weight that is left is one fp16 value, or two parts, over itself; the others are below 2^-57)
+            assert bool((off <= (half + 2.0 ** -21) * want.abs()[far] + 2.0 ** -40).all())
+    assert clear > 0.99 * rows
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("rows,B,H", [(1, 1, 1), (1, 1, 300), (1, 70, 32), (70, 1, 1), (70, 20, 20), (129, 32, 12)])
+def test_scores_whose_steps_are_eight(rows, B, H, dtype):
+    """Half of the pages have scores of 2^26 (in powers of two), where binary32 counts in eights, the others 2^26 + 8."""
+    n = 8 if B * H >= 2048 else 16
+    cache = paged.Cache(1, H, n)
+    params = paged.Params(1, H, H, None, dtype, softmax_scale=math.log(2.0))
+    k, v, s = cache.values()
+    k.zero_()
+    for d, value in ((0, 256.0), (1, 2.0 ** -5)):
+        k[:, :, (0 if d == 0 else n // 2):, :, d] = torch.full((), value, device=DEV).to(k.dtype)
+    v[:, :, :n // 2] = torch.ones_like(v[:, :, :n // 2])
+    v[:, :, n // 2:] = (torch.ones(v[:, :, n // 2:].shape, device=DEV) * 3).to(v.dtype)
+    s[..., 0], s[..., 1] = 2.0 ** 5, 1.0
+    q = torch.zeros((1, B * rows, H, 64), dtype=dtype, device=DEV)
+    q[..., 0], q[..., 1] = 2.0 ** 13, 8.0
+    got = paged.attend(params, cache, q, i32([64 * n - 1] * (B * rows)), i32(list(range(0, B * rows + 1, rows))),
+                       i32([list(range(n))] * B), i32([64 * n] * B), rows, 64 * n)
+    want = (1.0 * 2.0 ** -8 + 3.0) / (2.0 ** -8 + 1.0)
+    assert float((got.double() - want).abs().max()) <= (2 * 2.0 ** -11 + 1088 * 2.0 ** -23 + torch.finfo(dtype).eps / 2) * want
 
 
 # ----------------------------------------------------------- value scales
