@@ -8,7 +8,7 @@ import torch
 
 import paged_ref as ref
 from paper_2603_26110_amd import paged
-from test_gpu_paged import BF16, DEV, F16, F32, World, i32
+from test_gpu_paged import BF16, DEV, F16, F32, SHAPES, World, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -129,6 +129,62 @@ def test_scores_whose_steps_are_eight(rows, B, H, dtype):
                        i32([list(range(n))] * B), i32([64 * n] * B), rows, 64 * n)
     want = (1.0 * 2.0 ** -8 + 3.0) / (2.0 ** -8 + 1.0)
     assert float((got.double() - want).abs().max()) <= (2 * 2.0 ** -11 + 1088 * 2.0 ** -23 + torch.finfo(dtype).eps / 2) * want
+
+
+# ------------------------------------------------ types, bounds, row offsets
+OTHERS = [(F16, "none", False), (F16, "half", False), (F16, "half", True), (BF16, "none", False), (BF16, "pairs", False),
+          (BF16, "none", True), (F32, "half", False), (F32, "pairs", False)]
+
+
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+@pytest.mark.parametrize("dtype,rope,out_f32", OTHERS)
+def test_attend_of_the_other_types(shape, dtype, rope, out_f32):
+    w = World(*SHAPES[shape], dtype=dtype, rope=rope, out_f32=out_f32, fused=shape % 2 == 0, layers=1 + shape % 2, seed=50 + shape)
+    for causal in (True, False):
+        w.check(w.call(causal), causal)
+
+
+@pytest.mark.parametrize("kind", list(ALL))
+@pytest.mark.parametrize("dtype,rope,out_f32", OTHERS)
+def test_every_launch_of_the_other_types(kind, dtype, rope, out_f32):
+    w = World(*ALL[kind], dtype=dtype, rope=rope, out_f32=out_f32, seed=37)
+    for causal in (True, False):
+        w.check(w.call(causal), causal)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_bounds_that_are_not_reached(dtype):
+    # a serving loop gives its capacity: other kernels and splits, the same result within its bound
+    w = World([300, 5, 64, 1025], [1, 4, 0, 2], 6, 2, dtype=dtype, seed=38)
+    for max_new in (4, 40, 1000):
+        for max_len in (1025, 4000, 100_000, 2 ** 30):
+            for causal in (True, False):
+                w.check(w.call(causal, max_new=max_new, max_len=max_len), causal)
+
+
+@pytest.mark.parametrize("new", [1, 40, 200])
+def test_rows_that_row0_puts_outside_are_not_written(new):
+    lens, news = [400, 300, 200, 250, 220], [new, min(new, 300), min(new, 200), min(new, 3), min(new, 220)]
+    w = World(lens, news, 4, 2, seed=39)
+    fine = w.call()
+    w.check(fine)
+
+    def rows(row0, untouched):
+        out = torch.full_like(fine, 7.0)
+        w.call(row0=i32(row0), out=out)
+        for b in range(5):
+            at = slice(w.row0[b], w.row0[b + 1])
+            if b in untouched:
+                assert bool((out[:, at] == 7).all()), b
+            else:
+                assert torch.equal(out[:, at], fine[:, at]), b
+    rows(w.row0, ())
+    # a first row before the rows, a last one behind them: those sequences are skipped, the others are not
+    rows([-1] + w.row0[1:5] + [w.rows + 1], (0, 4))
+    rows([-2 ** 31] + w.row0[1:5] + [2 ** 31 - 1], (0, 4))
+    # everything behind the rows, or before them
+    rows([w.rows + 5] * 6, range(5))
+    rows([-7] * 6, range(5))
 
 
 # ----------------------------------------------------------- value scales
