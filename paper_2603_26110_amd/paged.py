@@ -177,7 +177,20 @@ class Params:
         object.__setattr__(self, "_out", torch.float32 if self.flags & OUT_FP32 else self.io_dtype)
 
 
-class Cache:
+class _Kept:
+    """Attributes that stay as the constructor leaves them, ``_c`` (the buffers' addresses) the last of them: the
+    buffers' contents may change, the buffers may not."""
+
+    def __setattr__(self, name, value):
+        if "_c" in self.__dict__:
+            raise AttributeError(f"{name} of a {type(self).__name__} cannot be set: make another")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{name} of a {type(self).__name__} cannot be deleted")
+
+
+class Cache(_Kept):
     """Pages in device memory: per (layer, key/value head, page) 4096 key codes, 4096 value codes and two scales.
     ``buffers``: the caller's own (k_codes, v_codes, scales) in place of new, zeroed ones."""
 
@@ -210,7 +223,7 @@ class Cache:
         return self._values
 
 
-class PagePool:
+class PagePool(_Kept):
     """The free pages of a cache, on the GPU: at first all of them, page 0 the first to go out."""
 
     def __init__(self, pages: int, device="cuda"):

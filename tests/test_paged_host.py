@@ -236,3 +236,20 @@ def test_reference_pool_gives_back_what_it_took():
         state.release([n - m * ok for n, m, ok in zip(state.len, new, granted)])
         assert before == (state.stack, state.table, state.len)
         state.assign([1] * 6, 6, 30)
+
+
+def test_a_cache_and_a_pool_keep_their_buffers():
+    # (the library is given their addresses as they were made)
+    cache, pool = paged.Cache(2, 3, 5, device="cpu"), paged.PagePool(5, device="cpu")
+    for thing, names in ((cache, ("k_codes", "v_codes", "scales", "pages", "num_layers", "kv_heads", "device")),
+                         (pool, ("stack", "state", "pages", "device"))):
+        for name in names:
+            was = getattr(thing, name)
+            with pytest.raises(AttributeError):
+                setattr(thing, name, was.clone() if isinstance(was, torch.Tensor) else was)
+            with pytest.raises(AttributeError):
+                delattr(thing, name)
+            assert getattr(thing, name) is was
+    pool.state[0] = 3                              # what they hold may change
+    cache.scales[..., 1] *= 2
+    assert pool.state[0] == 3 and float(cache.scales[0, 0, 0, 1]) == 2.0 ** -47
