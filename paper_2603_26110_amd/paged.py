@@ -300,21 +300,24 @@ def _model_checks(params: Params, cache: Cache) -> int:
     return index
 
 
-def append(params: Params, cache: Cache, k, v, slots, pos, layer0: int = 0) -> None:
+def append(params: Params, cache: Cache, k, v, slots, pos=None, layer0: int = 0) -> None:
     """Quantizes k, v [nlayers][rows][kv_heads][64] into the cache (tqp_append). ``slots`` int64 [rows] and ``pos``
-    int32 [rows] come from assign(). k and v may be slices (strides in multiples of 8 elements)."""
+    int32 [rows] come from assign(); without rope_cs no ``pos`` is needed. k and v may be slices (strides in multiples
+    of 8 elements)."""
     L = _lib or _load()
     index = _model_checks(params, cache)
     io, heads = params.io_dtype, params.kv_heads
+    no_pos = pos is None and params.rope_cs is None
     try:
         shape = k.shape
         rows = shape[1]
-        fine = (k.dtype is io and v.dtype is io and slots.dtype is torch.int64 and pos.dtype is torch.int32
+        fine = (k.dtype is io and v.dtype is io and slots.dtype is torch.int64
                 and len(shape) == 4 and shape[3] == 64 and shape[2] == heads and v.shape == shape
-                and k.stride(3) == 1 and v.stride(3) == 1 and slots.is_contiguous() and pos.is_contiguous()
+                and k.stride(3) == 1 and v.stride(3) == 1 and slots.is_contiguous()
                 and index >= 0 and k.get_device() == index and v.get_device() == index
-                and slots.get_device() == index and pos.get_device() == index
-                and slots.numel() >= rows and pos.numel() >= rows)
+                and slots.get_device() == index and slots.numel() >= rows
+                and (no_pos or (pos.dtype is torch.int32 and pos.is_contiguous() and pos.get_device() == index
+                                and pos.numel() >= rows)))
     except (AttributeError, IndexError):
         fine = False
     if not fine:
@@ -323,9 +326,11 @@ def append(params: Params, cache: Cache, k, v, slots, pos, layer0: int = 0) -> N
         if k.shape != v.shape:
             raise ValueError("k and v must have the same shape")
         _dev(slots, "slots", torch.int64, index, rows)
-        _dev(pos, "pos", torch.int32, index, rows)
+        if not no_pos:
+            _dev(pos, "pos", torch.int32, index, rows)
     _check(_launch(index, L.tqp_append, ctypes.byref(params._c), ctypes.byref(cache._c), ctypes.byref(_rows(k, shape)),
-                   ctypes.byref(_rows(v, shape)), rows, layer0, shape[0], slots.data_ptr(), pos.data_ptr()))
+                   ctypes.byref(_rows(v, shape)), rows, layer0, shape[0], slots.data_ptr(),
+                   None if no_pos else pos.data_ptr()))
 
 
 def workspace_bytes(params: Params, nlayers: int, B: int, max_new: int, max_len: int) -> int:

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paged_ref as ref
+import paper_2603_26110_amd as tq
 from paper_2603_26110_amd import paged
 from test_gpu_paged import BF16, DEV, F16, F32, SHAPES, World, i32
 
@@ -264,3 +265,24 @@ def test_assign_of_as_many_rows_as_there_are_numbers():
         assert bool((t[:before] == 7).all())
         for i in range(before + 75, before + rows, 1 << 28):
             assert bool((t[i:i + (1 << 28)] == -1).all())
+
+
+# ----------------------------------------------------------------- append
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_append_without_rope_needs_no_positions(dtype):
+    g = torch.Generator(device=DEV).manual_seed(41)
+    k, v = torch.randn((2, 1, 150, 2, 64), generator=g, device=DEV).to(dtype).unbind(0)
+    slots, pos = torch.arange(64, 214, device=DEV), i32(list(range(150)))
+    params = paged.Params(1, 4, 2, None, dtype)
+    caches = [paged.Cache(1, 2, 4) for _ in range(3)]
+    paged.append(params, caches[0], k, v, slots, pos)
+    paged.append(params, caches[1], k, v, slots, None)
+    paged.append(params, caches[2], k, v, slots)
+    for c in caches[1:]:
+        for name in ("k_codes", "v_codes", "scales"):
+            assert torch.equal(getattr(c, name), getattr(caches[0], name)), name
+    assert bool(caches[0].k_codes.any())
+    with pytest.raises(TypeError):                # (with RoPE they are needed)
+        paged.append(paged.Params(1, 4, 2, tq.rope_table(200), dtype), caches[0], k, v, slots)
+    with pytest.raises(ValueError):               # (and what is given is looked at)
+        paged.append(params, caches[0], k, v, slots, pos[:149])
