@@ -99,6 +99,12 @@ def _check(status: int) -> None:
         raise TQError(f"status {status}: {last_error()}")
 
 
+def _fit(*numbers) -> None:
+    """Raises unless all numbers are 32-bit ones (ctypes would cut them to that)."""
+    if max(numbers) >= 2 ** 31 or min(numbers) < -2 ** 31:
+        raise ValueError(f"{[n for n in numbers if not -2 ** 31 <= n < 2 ** 31]}: past 32 bits")
+
+
 # A call's marshalling is a good part of a small launch's time (9 us of host work
 # per append against 4 us of kernel, before): the checks of a call's tensors are
 # one expression, and only where that fails do they run one by one, in order, to
@@ -170,6 +176,7 @@ class Params:
             _dev(cs, "rope_cs", torch.float32)
             if cs.dim() != 3 or tuple(cs.shape[1:]) != (32, 2):
                 raise ValueError("rope_cs must be [positions][32][2]")
+        _fit(self.num_layers, self.num_heads, self.kv_heads, self.flags)
         c = _Params(64, self.num_layers, self.num_heads, self.kv_heads, _IO[self.io_dtype], self.flags,
                     self.softmax_scale, 0 if cs is None else cs.shape[0], None if cs is None else cs.data_ptr())
         object.__setattr__(self, "_c", c)
@@ -237,6 +244,7 @@ class PagePool(_Kept):
 
 
 def cache_bytes(num_layers: int, kv_heads: int, pages: int) -> int:
+    _fit(num_layers, kv_heads)
     return int(_load().tqp_cache_bytes(num_layers, kv_heads, pages))
 
 
@@ -268,6 +276,7 @@ def assign(pool: PagePool, table, seq_len, new_tokens, rows: int, out=None):
     L = _lib or _load()
     B = _pool_checks(pool, table, seq_len, new_tokens, "new_tokens")
     rows = int(rows)
+    _fit(rows, B, table.shape[1])
     if out is None:
         out = (torch.empty(rows, dtype=torch.int64, device=pool.device),
                *torch.empty(rows + B + 1 + B, dtype=torch.int32, device=pool.device).split_with_sizes((rows, B + 1, B)))
@@ -286,6 +295,7 @@ def release(pool: PagePool, table, seq_len, keep) -> None:
     """Cuts every sequence to min(keep, seq_len) tokens and takes the pages it no longer needs back (tqp_release)."""
     L = _lib or _load()
     B = _pool_checks(pool, table, seq_len, keep, "keep")
+    _fit(B, table.shape[1])
     _check(_launch(pool._index, L.tqp_release, ctypes.byref(pool._c), table.data_ptr(), table.shape[1], B,
                    seq_len.data_ptr(), keep.data_ptr()))
 
@@ -328,6 +338,7 @@ def append(params: Params, cache: Cache, k, v, slots, pos=None, layer0: int = 0)
         _dev(slots, "slots", torch.int64, index, rows)
         if not no_pos:
             _dev(pos, "pos", torch.int32, index, rows)
+    _fit(rows, layer0, shape[0])
     _check(_launch(index, L.tqp_append, ctypes.byref(params._c), ctypes.byref(cache._c), ctypes.byref(_rows(k, shape)),
                    ctypes.byref(_rows(v, shape)), rows, layer0, shape[0], slots.data_ptr(),
                    None if no_pos else pos.data_ptr()))
@@ -335,6 +346,7 @@ def append(params: Params, cache: Cache, k, v, slots, pos=None, layer0: int = 0)
 
 def workspace_bytes(params: Params, nlayers: int, B: int, max_new: int, max_len: int) -> int:
     """Bytes of the workspace that attend() needs for these sizes (0 for most)."""
+    _fit(nlayers, B, max_new, max_len)
     return int(_load().tqp_workspace_bytes(ctypes.byref(params._c), nlayers, B, max_new, max_len))
 
 
@@ -367,6 +379,8 @@ def attend(params: Params, cache: Cache, q, pos, row0, table, seq_len, max_new: 
         _dev(pos, "pos", i32, index, q.shape[1])
         _dev(row0, "row0", i32, index, table.shape[0] + 1)
         _dev(seq_len, "seq_len", i32, index, table.shape[0])
+    max_new, max_len = int(max_new), int(max_len)
+    _fit(rows, B, table.shape[1], layer0, shape[0], max_new, max_len)
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=cache.device)
     else:
@@ -381,11 +395,11 @@ def attend(params: Params, cache: Cache, q, pos, row0, table, seq_len, max_new: 
             raise ValueError("workspace must be contiguous")
         size = workspace.numel() * workspace.element_size()
     args = (ctypes.byref(params._c), ctypes.byref(cache._c), ctypes.byref(_rows(q, shape)), rows, B, layer0, shape[0],
-            pos.data_ptr(), row0.data_ptr(), table.data_ptr(), table.shape[1], seq_len.data_ptr(), int(max_new),
-            int(max_len), 1 if causal else 0, out.data_ptr())
+            pos.data_ptr(), row0.data_ptr(), table.data_ptr(), table.shape[1], seq_len.data_ptr(), max_new,
+            max_len, 1 if causal else 0, out.data_ptr())
     status = _launch(index, L.tqp_attend, *args, None if workspace is None else workspace.data_ptr(), size)
     if status == _CAPACITY:              # (refused before anything was launched)
-        need = L.tqp_workspace_bytes(args[0], shape[0], B, int(max_new), int(max_len))
+        need = L.tqp_workspace_bytes(args[0], shape[0], B, max_new, max_len)
         if need > size:
             workspace = torch.zeros(need, dtype=torch.uint8, device=cache.device)
             status = _launch(index, L.tqp_attend, *args, workspace.data_ptr(), need)

@@ -286,3 +286,24 @@ def test_append_without_rope_needs_no_positions(dtype):
         paged.append(paged.Params(1, 4, 2, tq.rope_table(200), dtype), caches[0], k, v, slots)
     with pytest.raises(ValueError):               # (and what is given is looked at)
         paged.append(params, caches[0], k, v, slots, pos[:149])
+
+
+def test_numbers_past_32_bits_are_refused_not_cut():
+    w = World([100, 70], [2, 1], 4, 2, seed=42)
+    before = w.call()
+    kv = torch.zeros((1, w.rows, 2, 64), dtype=F16, device=DEV)
+    slots, out = torch.full((w.rows,), -1, dtype=torch.int64, device=DEV), torch.full_like(before, 7.0)
+    for wide in (2 ** 31, 2 ** 32, 2 ** 32 + 100, -2 ** 32):
+        for kw in (dict(max_new=wide), dict(max_len=wide), dict(layer0=wide)):
+            with pytest.raises(ValueError):
+                w.call(out=out, **kw)
+        with pytest.raises(ValueError):
+            paged.append(w.params, w.cache, kv, kv, slots, i32(w.pos), layer0=wide)
+        pool, table, lens = paged.PagePool(9), torch.full((2, 4), -1, dtype=torch.int32, device=DEV), i32([0, 0])
+        room = (torch.empty(8, dtype=torch.int64, device=DEV), i32([0] * 8), i32([0] * 3), i32([0] * 2))
+        with pytest.raises(ValueError):
+            paged.assign(pool, table, lens, i32([2, 1]), wide, out=room)
+        assert pool.state.tolist() == [9, 0, 0, 0] and lens.tolist() == [0, 0]
+    assert bool((out == 7).all())
+    with pytest.raises(tq.TQError):                # (what 32 bits hold the library itself refuses)
+        w.call(layer0=-1)

@@ -253,3 +253,22 @@ def test_a_cache_and_a_pool_keep_their_buffers():
     pool.state[0] = 3                              # what they hold may change
     cache.scales[..., 1] *= 2
     assert pool.state[0] == 3 and float(cache.scales[0, 0, 0, 1]) == 2.0 ** -47
+
+
+def test_numbers_past_32_bits_are_refused_not_cut():
+    wide = 2 ** 32 + 1                             # (1 in 32 bits)
+    for kw in (dict(num_layers=wide), dict(num_heads=wide), dict(kv_heads=wide), dict(num_layers=-2 ** 32 + 1),
+               dict(flags=2 ** 32)):
+        with pytest.raises(ValueError):
+            paged.Params(**{**dict(num_layers=1, num_heads=1, kv_heads=1), **kw})
+    params = paged.Params(1, 1, 1)
+    for i in range(4):
+        sizes = [1, 1, 1, 100_000]
+        assert paged.workspace_bytes(params, *sizes) > 0
+        sizes[i] = wide
+        with pytest.raises(ValueError):
+            paged.workspace_bytes(params, *sizes)
+    for args in ((wide, 1, 1), (1, wide, 1)):
+        with pytest.raises(ValueError):
+            paged.cache_bytes(*args)
+    assert paged.cache_bytes(1, 1, 2 ** 33) == 2 ** 33 * 8200
