@@ -36,6 +36,7 @@ __all__ = ["Params", "Cache", "PagePool", "assign", "release", "append", "attend
 
 PAGE, MAX_SEQS = 64, 4096
 _CAPACITY = -5
+_COUNTERS = 16384                        # bytes at the start of a workspace that must be zero before its first use
 _IO = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 lib_path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libturboesm_paged.so")
@@ -354,9 +355,9 @@ def attend(params: Params, cache: Cache, q, pos, row0, table, seq_len, max_new: 
            layer0: int = 0, out=None, workspace=None) -> torch.Tensor:
     """Attention of the query rows q [nlayers][rows][num_heads][64] over the pages (tqp_attend): row t of sequence b
     sees the sequence's tokens j < seq_len[b], and with ``causal`` those up to its own position. ``max_new`` and
-    ``max_len`` bound the rows and tokens of a sequence. ``workspace``: a tensor of workspace_bytes(...) bytes, zeroed
-    before its first use (without one that is large enough a new one is made). Returns out
-    [nlayers][rows][num_heads][64]."""
+    ``max_len`` bound the rows and tokens of a sequence. ``workspace``: a tensor of workspace_bytes(...) bytes whose
+    first 16384 are zero before its first use (without one that is large enough every call makes a new one). Returns
+    out [nlayers][rows][num_heads][64]."""
     L = _lib or _load()
     index = _model_checks(params, cache)
     io, heads, i32, dtype = params.io_dtype, params.num_heads, torch.int32, params._out
@@ -401,7 +402,8 @@ def attend(params: Params, cache: Cache, q, pos, row0, table, seq_len, max_new: 
     if status == _CAPACITY:              # (refused before anything was launched)
         need = L.tqp_workspace_bytes(args[0], shape[0], B, max_new, max_len)
         if need > size:
-            workspace = torch.zeros(need, dtype=torch.uint8, device=cache.device)
+            workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+            workspace[:_COUNTERS].zero_()
             status = _launch(index, L.tqp_attend, *args, workspace.data_ptr(), need)
     _check(status)
     return out

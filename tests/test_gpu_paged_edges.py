@@ -307,3 +307,32 @@ def test_numbers_past_32_bits_are_refused_not_cut():
     assert bool((out == 7).all())
     with pytest.raises(tq.TQError):                # (what 32 bits hold the library itself refuses)
         w.call(layer0=-1)
+
+
+# -------------------------------------------------------------- workspace
+def test_only_the_counters_of_a_workspace_are_cleared():
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Fills(TorchDispatchMode):
+        """Bytes that calls set to a value."""
+        total = 0
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            out = func(*args, **(kwargs or {}))
+            if func.overloadpacket.__name__ in ("zeros", "zero_", "fill_", "full"):
+                self.total += out.numel() * out.element_size()
+            return out
+
+    for w in (World([9000], [70], 2, 1, seed=43), World([8192], [1], 4, 1, seed=44)):
+        need = paged.workspace_bytes(w.params, 1, 1, w.new[0], w.lens[0])
+        want = w.call()
+        w.check(want)
+        args = dict(pos=i32(w.pos), row0=i32(w.row0), table=i32(w.table), seq_len=i32(w.lens))
+        for size in (None, 1000):
+            with Fills() as fills:
+                got = w.call(workspace=None if size is None else torch.empty(size, dtype=torch.uint8, device=DEV), **args)
+            assert torch.equal(got, want) and 0 < fills.total <= 16384 < need
+        room = torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV)      # (what lies behind them may hold anything)
+        room[:16384] = 0
+        for _ in range(3):
+            assert torch.equal(w.call(workspace=room), want) and int(room[:16384].count_nonzero()) == 0
