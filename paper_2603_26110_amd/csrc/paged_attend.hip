@@ -381,7 +381,9 @@ __device__ void join_parts(const AttendArgs& a, const Sequence& s, int l, int h,
 
 __device__ __forceinline__ void store_part(float* p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void store_part(float* p, f32x4 x) {
-  asm volatile("global_store_dwordx4 %0, %1, off sc1" ::"v"(p), "v"(x) : "memory");   // (as the store above, four at a time)
+  // (as the store above, four at a time; the compiler does not see that a store of
+  // more than two words is here, whose data may be written again one wait state later)
+  asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 0" ::"v"(p), "v"(x) : "memory");
 }
 
 // ------------------------------------------------------------- few rows

@@ -11,7 +11,7 @@ import torch
 
 import paged_ref as ref
 from paper_2603_26110_amd import TQError, paged
-from test_code_hazards import OBJDUMP, _code_objects, too_early
+from test_code_hazards import OBJDUMP, _code_objects, _registers, too_early
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.skipif(not os.path.exists(paged.lib_path), reason="libturboesm_paged.so is not built")
@@ -272,3 +272,37 @@ def test_numbers_past_32_bits_are_refused_not_cut():
         with pytest.raises(ValueError):
             paged.cache_bytes(*args)
     assert paged.cache_bytes(1, 1, 2 ** 33) == 2 ** 33 * 8200
+
+
+def stores_whose_data_is_written_next(listing):
+    """(store, writer) of the stores of more than two words whose data the very next instruction writes (gfx9 wants a
+    wait state between them, which the compiler keeps for its own stores but not for those in assembly)."""
+    lines = [ln.split("//")[0].strip() for ln in listing.splitlines() if ln.startswith("\t")]
+    found = []
+    for store, after in zip(lines, lines[1:]):
+        if re.match(r"(global|flat|scratch)_store_dwordx[34]\b", store) and after.startswith("v_"):
+            data = _registers(store.split(",")[1].strip())
+            if set(data) & set(_registers(after.partition(" ")[2].split(",")[0].strip())):
+                found.append((store, after))
+    return found
+
+
+def test_no_store_loses_its_data(tmp_path):
+    code = "\tglobal_store_dwordx4 v[0:1], v[4:7], off sc1   // 0:\n{}\tv_mov_b32_e32 v7, 0   // 8:\n"
+    assert len(stores_whose_data_is_written_next(code.format(""))) == 1
+    assert not stores_whose_data_is_written_next(code.format("\ts_nop 0\n"))
+    if not os.path.exists(OBJDUMP):
+        pytest.skip("llvm-objdump is missing")
+    ours = 0
+    for i, obj in enumerate(_code_objects(paged.lib_path)):
+        path = tmp_path / f"{i}.o"
+        path.write_bytes(obj)
+        listing = subprocess.run([OBJDUMP, "-d", "--mcpu=gfx950", "--no-show-raw-insn", str(path)], capture_output=True,
+                                 text=True, check=True).stdout
+        assert not stores_whose_data_is_written_next(listing)
+        lines = [ln.split("//")[0].strip() for ln in listing.splitlines() if ln.startswith("\t")]
+        for store, after in zip(lines, lines[1:]):
+            if re.match(r"global_store_dwordx4 .* sc1$", store):
+                ours += 1
+                assert re.match(r"s_nop", after), (store, after)
+    assert ours > 0
