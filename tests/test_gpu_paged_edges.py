@@ -9,7 +9,7 @@ import torch
 import paged_ref as ref
 import paper_2603_26110_amd as tq
 from paper_2603_26110_amd import paged
-from test_gpu_paged import BF16, DEV, F16, F32, SHAPES, World, i32
+from test_gpu_paged import BF16, DEV, F16, F32, SHAPES, World, i32, random_cache, same_cache
 
 pytestmark = pytest.mark.gpu
 
@@ -336,3 +336,34 @@ def test_only_the_counters_of_a_workspace_are_cleared():
         room[:16384] = 0
         for _ in range(3):
             assert torch.equal(w.call(workspace=room), want) and int(room[:16384].count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("case", range(6))
+def test_append_across_many_skipped_rows(case, rope):
+    """Runs of one page with thousands of skipped rows before, between and behind them, and other pages around."""
+    gap = lambda n: [-1] * n
+    slots = [[64] + gap(5000) + [65],
+             gap(3000) + [64, 65, 66] + gap(1023) + [67] + gap(1025) + list(range(68, 128)) + gap(2000),
+             list(range(192, 256)) + [130] + gap(4095) + [131, 132, 64] + gap(4096) + [65],
+             [64 + i for i in range(10)] + gap(70000) + [74, 75] + gap(10) + [200],
+             gap(2048) + [64] + gap(63) + [65] + gap(64) + [66] + gap(1984) + [320],
+             [7 * 64 + 5] + gap(1500) + [10 ** 9, -5] + gap(1500) + [7 * 64 + 6] + gap(1100)][case]
+    g = torch.Generator(device=DEV).manual_seed(60 + case)
+    pages, N = 9, len(slots)
+    pos = [i % 90 for i in range(N)]
+    for i in range(0, N, 7):                       # (rows that only their position skips)
+        if slots[i] < 0 and rope:
+            slots[i], pos[i] = 3, (-1, 100)[i % 2]
+    cache = random_cache(1, 2, pages, case)
+    want = ref.CacheRef(cache)
+    size = 2.0 ** torch.randint(-9, 6, (1, N, 1, 1), generator=g, device=DEV).float()
+    k, v = (torch.randn((2, 1, N, 2, 64), generator=g, device=DEV) * size).unbind(0)
+    cs = tq.rope_table(100) if rope else None
+    paged.append(paged.Params(1, 2, 2, cs, F32), cache, k, v, torch.tensor(slots, device=DEV), i32(pos))
+    live = [i for i in range(N) if 0 <= slots[i] < 64 * pages and 0 <= pos[i] < 100]
+    # (one row after each is enough of a gap for the plain form)
+    keep = sorted({j for i in live for j in (i, min(i + 1, N - 1))})
+    want.append(k[:, keep].cpu().numpy(), v[:, keep].cpu().numpy(), [slots[i] for i in keep], [pos[i] for i in keep],
+                None if cs is None else cs.cpu().numpy(), False)
+    same_cache(cache, want)
