@@ -20,12 +20,13 @@
 // Measured: 640 (sequence, head) of 8192 tokens (671 MB) 119 us, 5.6 TB/s, where
 // a plain read of as much takes 111; 660 of 1025 tokens 19 us; 20 of 1025 tokens
 // 9 us, a chain of latencies. Every token of 1024 with every other in 33 layers
-// of 20 heads (177 GFLOP): 310 to 340 us, up to 570 TFLOP/s (a library product
-// of 8192^3: 1168).
+// of 20 heads (177 GFLOP): 296 to 313 us, up to 600 TFLOP/s (a library product
+// of 8192^3: 1168); with bf16 results 245.
 //
 // Rounding: q' and the weights round to fp16 (2^-11). That is 8 times finer
 // than a bf16 output; for an fp16 output q' is taken in two parts (the error
-// of a score grows with the score), for an fp32 output the weights too.
+// of a score grows with the score), for an fp32 output the weights too. An
+// fp16 query without RoPE is exact in one part.
 #include <algorithm>
 
 #include "paged_device.hpp"
@@ -635,9 +636,9 @@ __global__ __launch_bounds__(W * 64, PREC == 0 ? 4 : 3) void attend_few(AttendAr
 // waves, 64 rows a block, that take every other page each and are joined at the
 // end: twice the blocks and half the pages one after the other, for calls that
 // do not fill the chip. Two groups have one buffer each and a second barrier, so
-// that three blocks fit a compute unit, not two (16-bit results: four chunks 82 ->
-// 74 us, 20 heads of 8 ragged sequences of up to 500 tokens 37 -> 32, one prompt of
-// 1024 20.5 -> 20.9); with fp32 results they keep two (38 us against 42 for two
+// that three blocks fit a compute unit, not two (16-bit results: four chunks 81 ->
+// 75 us, 20 heads of 8 ragged sequences of up to 500 tokens 28 -> 25 a call, one prompt
+// of 1024 20.0 -> 20.3); with fp32 results they keep two (38 us against 42 for two
 // sequences of 1000).
 //
 // Values are converted over the reference scale of the output's sums, times the
@@ -997,7 +998,7 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   // Where blocks differ, by what their rows see or by their sequences' lengths, and
   // there are units enough (64 ragged prompts of 20 heads, 1280 units: causal 223
   // -> 200 us, else 352 -> 310; one sequence of 660 units, not causal, would go 344
-  // -> 356; four chunks on top of long sequences, 32 units, with two buffers 79 -> 134).
+  // -> 356; four chunks on top of long sequences, 32 units, took 134 so).
   g.spread = !p.few && (a.causal || a.B > 1) && g.units >= 64 * kXcds;
   const int64_t lines = g.by_xcd ? (g.units + kXcds - 1) / kXcds * kXcds : g.units;
   const dim3 grid((unsigned)(lines * p.tiles * p.nsplit)), block(p.waves * 64);

@@ -12,14 +12,17 @@ A serving loop:
 
     pool, cache = paged.PagePool(pages), paged.Cache(L, kv_heads, pages)
     table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+    room = torch.zeros(paged.workspace_bytes(params, 1, B, max_new, max_len), dtype=torch.uint8, device="cuda")
     slots, pos, row0, granted = paged.assign(pool, table, seq_len, new_tokens, rows)
     for l in range(L):                     # q, k, v: [1][rows][heads][64], rows of all sequences packed
         paged.append(params, cache, k, v, slots, pos, layer0=l)
-        out = paged.attend(params, cache, q, pos, row0, table, seq_len, max_new, max_len, layer0=l)
+        out = paged.attend(params, cache, q, pos, row0, table, seq_len, max_new, max_len, layer0=l, workspace=room)
     paged.release(pool, table, seq_len, keep)     # keep[b] = 0 where a sequence is finished
 
-Every call goes to the current stream of its tensors' device, never
-synchronizes, and can be captured into a graph.
+max_new and max_len are bounds that choose how attend runs: the closer they are
+to the longest sequence's rows and tokens the better. Every call goes to the
+current stream of its tensors' device, never synchronizes, and can be captured
+into a graph.
 """
 from __future__ import annotations
 
