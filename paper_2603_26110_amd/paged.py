@@ -189,16 +189,22 @@ class Params:
 
 
 class _Kept:
-    """Attributes that stay as the constructor leaves them, ``_c`` (the buffers' addresses) the last of them: the
-    buffers' contents may change, the buffers may not."""
+    """What the constructor sets stays, ``_c`` (the buffers' addresses) the last of it: the buffers' contents may change
+    (``cache.scales *= 2``), the buffers may not."""
+
+    _kept = frozenset()
 
     def __setattr__(self, name, value):
-        if "_c" in self.__dict__:
+        if name in self._kept and value is not self.__dict__[name]:
             raise AttributeError(f"{name} of a {type(self).__name__} cannot be set: make another")
         object.__setattr__(self, name, value)
+        if name == "_c":
+            object.__setattr__(self, "_kept", frozenset(self.__dict__) | {"_kept"})
 
     def __delattr__(self, name):
-        raise AttributeError(f"{name} of a {type(self).__name__} cannot be deleted")
+        if name in self._kept:
+            raise AttributeError(f"{name} of a {type(self).__name__} cannot be deleted: make another")
+        object.__delattr__(self, name)
 
 
 class Cache(_Kept):

@@ -246,7 +246,7 @@ def test_a_cache_and_a_pool_keep_their_buffers():
         for name in names:
             was = getattr(thing, name)
             with pytest.raises(AttributeError):
-                setattr(thing, name, was.clone() if isinstance(was, torch.Tensor) else was)
+                setattr(thing, name, was.clone() if isinstance(was, torch.Tensor) else object())
             with pytest.raises(AttributeError):
                 delattr(thing, name)
             assert getattr(thing, name) is was
@@ -306,3 +306,15 @@ def test_no_store_loses_its_data(tmp_path):
                 ours += 1
                 assert re.match(r"s_nop", after), (store, after)
     assert ours > 0
+
+
+def test_a_cache_and_a_pool_take_attributes_of_the_caller_s():
+    for thing in (paged.Cache(1, 1, 2, device="cpu"), paged.PagePool(2, device="cpu")):
+        thing.name = "mine"
+        thing.name += " too"
+        assert thing.name == "mine too"
+        del thing.name
+        assert not hasattr(thing, "name")
+    cache = paged.Cache(1, 1, 2, device="cpu")
+    cache.scales *= 2                              # (the tensor that is there already, changed in place)
+    assert float(cache.scales[0, 0, 0, 0]) == 2.0 ** -47
