@@ -372,24 +372,25 @@ def test_append_across_many_skipped_rows(case, rope):
 @pytest.mark.parametrize("lens,new,heads,kv_heads", [([8192, 300], [1, 1], 4, 1), ([9000, 100], [70, 80], 2, 1)])
 def test_a_captured_call_without_a_workspace(lens, new, heads, kv_heads):
     w = World(lens, new, heads, kv_heads, seed=45)
-    args = dict(pos=i32(w.pos), row0=i32(w.row0), table=i32(w.table), seq_len=i32(w.lens))
+    # (tensors made beforehand: a copy from the host cannot be captured)
+    args = (i32(w.pos), i32(w.row0), i32(w.table), i32(w.lens), max(new), max(lens))
     q, out = w.q.clone(), torch.empty_like(w.q)
     assert paged.workspace_bytes(w.params, 1, 2, max(new), max(lens)) > 0
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        w.call(q=q, out=out, **args)
+        paged.attend(w.params, w.cache, q, *args, out=out)
     torch.cuda.current_stream().wait_stream(side)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        w.call(q=q, out=out, **args)
+        paged.attend(w.params, w.cache, q, *args, out=out)
     g = torch.Generator(device=DEV).manual_seed(46)
     for i in range(5):
         q.copy_(torch.randn(q.shape, generator=g, device=DEV))
         out.fill_(7.0)
         graph.replay()
         got = out.clone()
-        assert torch.equal(got, w.call(q=q, **args)), i
+        assert torch.equal(got, paged.attend(w.params, w.cache, q, *args)), i
         if i % 2:
             torch.cuda.synchronize()
