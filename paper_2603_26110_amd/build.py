@@ -1,4 +1,4 @@
-"""Build libturboesm.so and libturboesm_paged.so (HIP, gfx950) in the package directory.
+"""Build libturboesm.so, libturboesm_paged.so and libturboesm_serve.so (HIP, gfx950) in the package directory.
 
     python -m paper_2603_26110_amd.build
 
@@ -19,10 +19,13 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libturboesm.so")
 LIB_PAGED = os.path.join(PKG, "libturboesm_paged.so")
+LIB_SERVE = os.path.join(PKG, "libturboesm_serve.so")
 SOURCES = ["tq_api.hip", "tq_quantize.hip", "tq_decode.hip", "tq_dequant.hip", "tq_calibrate.hip",
            "tq_probe.hip"]
 # The paged 8-bit cache is a library of its own, with a header of its own.
 SOURCES_PAGED = ["paged_api.hip", "paged_pages.hip", "paged_append.hip", "paged_attend.hip"]
+# So are the 4-bit one and the operators around it.
+SOURCES_SERVE = ["serve_api.hip", "serve_norm.hip", "serve_store.hip", "serve_attend.hip", "serve_verify.hip"]
 ARCH = os.environ.get("TQ_OFFLOAD_ARCH", "gfx950")
 
 CFLAGS = [
@@ -64,9 +67,10 @@ def _link(objs: list[str], lib: str) -> None:
 def build() -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
     with ThreadPoolExecutor(max_workers=4) as ex:
-        objs = list(ex.map(_compile, SOURCES + SOURCES_PAGED))
-    _link(objs[:len(SOURCES)], LIB)
-    _link(objs[len(SOURCES):], LIB_PAGED)
+        objs = list(ex.map(_compile, SOURCES + SOURCES_PAGED + SOURCES_SERVE))
+    for sources, lib in ((SOURCES, LIB), (SOURCES_PAGED, LIB_PAGED), (SOURCES_SERVE, LIB_SERVE)):
+        _link(objs[:len(sources)], lib)
+        del objs[:len(sources)]
     return LIB
 
 
