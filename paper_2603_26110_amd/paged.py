@@ -310,8 +310,10 @@ def release(pool: PagePool, table, seq_len, keep) -> None:
                    seq_len.data_ptr(), keep.data_ptr()))
 
 
-def _model_checks(params: Params, cache: Cache) -> int:
-    """The GPU of a call, once params and cache belong together."""
+def _model_checks(params: Params, cache: Cache, kind=Cache) -> int:
+    """The GPU of a call, once params and cache belong together. (A cache of another kind has other planes.)"""
+    if type(cache) is not kind and not isinstance(cache, kind):
+        raise TypeError(f"cache must be a {kind.__name__}")
     index = cache._index
     if cache.num_layers != params.num_layers or cache.kv_heads != params.kv_heads:
         raise ValueError("the cache has other layers or heads than params")

@@ -121,11 +121,6 @@ def cache_bytes(num_layers: int, kv_heads: int, pages: int) -> int:
     return int(_load().tqs_cache_bytes(num_layers, kv_heads, pages))
 
 
-def _cache4(cache) -> None:
-    if type(cache) is not Cache4 and not isinstance(cache, Cache4):
-        raise TypeError("cache must be a Cache4")
-
-
 def norm_rope(params: Params, q, k, pos=None, q_weight=None, k_weight=None, eps: float = 1e-6, sections=None, out=None):
     """Norms every head of q [nlayers][rows][num_heads][64] and k [nlayers][rows][kv_heads][64] (divided by the root of
     the mean of its squares and eps, times ``q_weight`` or ``k_weight``, fp32 [nlayers][64] or None for ones) and
@@ -186,8 +181,7 @@ def append(params: Params, cache: Cache4, k, v, slots, pos=None, layer0: int = 0
     int32 [rows] come from paged.assign(); without rope_cs no ``pos`` is needed. k and v may be slices (strides in
     multiples of 8 elements)."""
     L = _lib or _load()
-    _cache4(cache)
-    index = _model_checks(params, cache)
+    index = _model_checks(params, cache, Cache4)
     io, heads = params.io_dtype, params.kv_heads
     _check_rows(k, "k", io, heads, index)
     _check_rows(v, "v", io, heads, index)
@@ -208,8 +202,7 @@ def read(params: Params, cache: Cache4, slots, layer0: int = 0, nlayers: int | N
     (tqs_read): (k, v), each [nlayers][rows][kv_heads][64] of the params' output type. Keys come rotated, as they were
     quantized. ``out``: the two tensors to write to."""
     L = _lib or _load()
-    _cache4(cache)
-    index = _model_checks(params, cache)
+    index = _model_checks(params, cache, Cache4)
     _dev(slots, "slots", torch.int64, index)
     rows = slots.numel()
     if nlayers is None:
@@ -267,8 +260,7 @@ def attend(params: Params, cache: Cache4, q, pos, row0, table, seq_len, max_new:
     first 16384 are zero before its first use (without one that is large enough every call makes a new one). Returns
     out [nlayers][rows][num_heads][64]."""
     L = _lib or _load()
-    _cache4(cache)
-    index = _model_checks(params, cache)
+    index = _model_checks(params, cache, Cache4)
     _check_rows(q, "q", params.io_dtype, params.num_heads, index)
     _dev(table, "table", torch.int32, index)
     if table.dim() != 2:
