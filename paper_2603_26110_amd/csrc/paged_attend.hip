@@ -54,31 +54,6 @@ __device__ __forceinline__ f16x8 halves8(uint32_t lo, uint32_t hi, float by = 1.
 
 __device__ __forceinline__ f16x2 half2_of(_Float16 a, _Float16 b) { return f16x2{a, b}; }
 
-// The power of two that a row is divided by, from its largest entry's bits: 2^14
-// to 2^15 in fp16 then, so that fp16's lowest step is 2^-38 of it and a large
-// channel takes no bits from the others (64 products with codes of 448 are below
-// 2^30). Rows of zeros, and what is no number, stay as they are, and so do fp16
-// entries that were not rotated: they are fp16 values.
-template <int IO, int ROPE>
-__device__ __forceinline__ int row_exponent(uint32_t amax) {
-  return (IO == kF16 && ROPE == kNone) || amax < 0x00800000u || amax >= kInfBits ? 0 : (int)(amax >> 23) - 127 - 14;
-}
-
-// x 2^-e in two steps (e may be -140 .. 113).
-__device__ __forceinline__ float over_pow2(float x, int e) {
-  return x * pow2(-(e >> 1)) * pow2(-(e - (e >> 1)));
-}
-
-template <int PREC>
-__device__ __forceinline__ void split8(const float* x, int e, f16x8& hi, f16x8& lo) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float v = over_pow2(x[i], e);
-    hi[i] = (_Float16)v;
-    if (PREC > 0) lo[i] = (_Float16)(v - (float)hi[i]);
-  }
-}
-
 // What a sum of products is multiplied by: positive and finite, so that masked
 // scores stay -infinity and zeros stay zero.
 __device__ __forceinline__ float score_scale(float row, float page) {

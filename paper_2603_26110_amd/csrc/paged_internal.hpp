@@ -103,6 +103,7 @@ struct AttendGrid {
 struct AttendPlan {
   bool few;
   int waves, groups, nsplit, tiles;   // tiles: row tiles of a unit
+  int rows;                    // of a tile (set for the 4-bit cache)
   int64_t units;               // (layer, sequence, key/value head, row tile)
   size_t workspace;
 };

@@ -23,7 +23,8 @@
 namespace tqp {
 namespace {
 
-constexpr int kRowsFew = 16, kRowsMany = 32;
+constexpr int kRowsMany = 32;
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 // The reference of the exponents is a score that was the largest when it was taken; it
 // moves when a score is 15 above it, so that rescaling is rare.
 constexpr float kRaise = 15.0f;
@@ -64,11 +65,30 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&part)[PARTS]
   }
 }
 
-// N entries of a query row in the Hadamard basis, over 8, as parts of eight entries an
-// operand. Lanes 64 / N .. hold the row together, lane i at i * (64 / (64 / N)) .. (the
-// lanes' numbers differ in bits FIRST, 2 FIRST, ..).
-template <int N, int FIRST, int PARTS>
-__device__ __forceinline__ void query_parts(float (&x)[N], bf16x8 (&q)[PARTS][N / 8]) {
+// Eight codes as fp16.
+__device__ __forceinline__ f16x8 codes_f16(uint32_t w) {
+  const u32x4 v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3))};
+  return __builtin_bit_cast(f16x8, v);
+}
+
+// Two words with the codes of four dimensions of two tokens each, as pairs of a token of
+// the first and of the second: dimension d of the first two in v[d][i], of the others in v[d][i + 2].
+__device__ __forceinline__ void codes_pairs(uint32_t first, uint32_t second, u32x4 (&v)[4], int i) {
+  const u32x4 a = __builtin_bit_cast(u32x4, codes_f16(first)), b = __builtin_bit_cast(u32x4, codes_f16(second));
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    v[0][2 * n + i] = __builtin_amdgcn_perm(b[2 * n], a[2 * n], 0x05040100);
+    v[1][2 * n + i] = __builtin_amdgcn_perm(b[2 * n], a[2 * n], 0x07060302);
+    v[2][2 * n + i] = __builtin_amdgcn_perm(b[2 * n + 1], a[2 * n + 1], 0x05040100);
+    v[3][2 * n + i] = __builtin_amdgcn_perm(b[2 * n + 1], a[2 * n + 1], 0x07060302);
+  }
+}
+
+// N entries of a query row in the Hadamard basis, over 8. Lanes whose numbers differ in
+// bits FIRST, 2 FIRST, .. hold the row together, in the order of these bits.
+template <int N, int FIRST>
+__device__ __forceinline__ void hadamard_query(float (&x)[N]) {
 #pragma unroll
   for (int n = 1; n < N; n *= 2)
 #pragma unroll
@@ -80,17 +100,22 @@ __device__ __forceinline__ void query_parts(float (&x)[N], bf16x8 (&q)[PARTS][N 
       }
 #pragma unroll
   for (int with = FIRST; with < 64; with *= 2) {
-    const float sign = threadIdx.x & with ? -1.0f : 1.0f;
+    const float sign = threadIdx.x & with ? -0.125f : 0.125f, own = with == 32 ? 0.125f : 1.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = fmaf(sign, x[i], __shfl_xor(x[i], with, 64));
+    for (int i = 0; i < N; ++i) x[i] = fmaf(with == 32 ? sign : sign * 8.0f, x[i], own * __shfl_xor(x[i], with, 64));
   }
+}
+
+// Such entries as parts of eight an operand.
+template <int N, int PARTS>
+__device__ __forceinline__ void query_parts(const float (&x)[N], bf16x8 (&q)[PARTS][N / 8]) {
 #pragma unroll
   for (int i = 0; i < N; i += 8) {
     u32x4 w[PARTS];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       uint32_t p[PARTS];
-      split2<PARTS>(x[i + 2 * j] * 0.125f, x[i + 2 * j + 1] * 0.125f, p);
+      split2<PARTS>(x[i + 2 * j], x[i + 2 * j + 1], p);
 #pragma unroll
       for (int n = 0; n < PARTS; ++n) w[n][j] = p[n];
     }
@@ -104,12 +129,34 @@ __device__ __forceinline__ void query_parts(float (&x)[N], bf16x8 (&q)[PARTS][N 
 __device__ __forceinline__ bool rounds_first(float top) { return __any(fabsf(top) > 0x1p20f && fabsf(top) < INFINITY); }
 
 // ------------------------------------------------------------- few rows
-template <int IO, int PARTS, int ROPE, int W>
-__global__ __launch_bounds__(W * 64, PARTS == 2 ? 4 : 3) void attend4_few(Attend4Args a, AttendGrid grid) {
+// S = Q K^T (A: queries, a row per row; B: keys, a token per column) and O = P V (A:
+// weights; B: values, a dimension per column): a lane has the scores of one token of
+// every 16 for four rows, so that a token's two scales are one lane's. They stay out of
+// the products: scores are multiplied by the key's, and a weight takes its value's along,
+//   P_j = exp2(s_j + log2 scale(v_j) - m),  l = sum_j P_j / scale(v_j),
+// with m near the largest of these exponents. So codes enter the matrix cores as they
+// are (fp16 holds them, and converts at twice bf16's rate), a weight's rounding to fp16 is
+// relative to the largest contribution, and l loses nothing: exponents of scales differ by
+// 95 at most, P of the largest score is 2^-95 or more.
+// Weights go through LDS, from a token a lane to the eight tokens of a row that a lane of
+// the second product takes: in the order in which the value plane has them.
+//
+// R: rows of a unit. Up to 4: the sixteen rows of the first product are the unit's rows four
+// times, and lane group g takes the scores of tokens 16 g .. 16 g + 15 only: a score a lane
+// and row instead of four.
+constexpr float kTop = 7.0f;                          // the largest weight is kept in 2^7 .. 2^15
+constexpr int kWeights = 64 * 2 + 16;                 // bytes of a row's weights in LDS, and some to spread the banks
+
+template <int IO, int WPARTS, int ROPE, int W, int R>
+__global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args a, AttendGrid grid) {
   constexpr int kStride = kDim + 4;
-  __shared__ float s_m[W][kRowsFew], s_l[W][kRowsFew];
-  static_assert(W == 1 || W * kStride >= 2 * kMaxSplit, "room for the splits' statistics");   // (one wave: no splits)
-  __shared__ __align__(16) float s_o[W * kRowsFew * kStride];
+  constexpr bool kPacked = R <= 4;
+  constexpr int kTokens = kPacked ? 1 : 4, kRows = R == 1 ? 1 : 4;   // scores of a lane
+  __shared__ float s_m[W][R], s_l[W][R];
+  static_assert(W == 1 || W * R * kStride >= 2 * R * kMaxSplit, "room for the splits' statistics");   // (one wave: no splits)
+  static_assert(WPARTS * kWeights <= kStride * 4 * 2, "room for a row's weights");
+  constexpr int kRoom = R * kStride * 4 > R * WPARTS * kWeights ? R * kStride : R * WPARTS * kWeights / 4;   // floats of a wave
+  __shared__ __align__(16) float s_o[W * kRoom];
   __shared__ int s_last;
   const Place place = place_of(a, grid);
   if (!place.there) return;
@@ -126,14 +173,16 @@ __global__ __launch_bounds__(W * 64, PARTS == 2 ? 4 : 3) void attend4_few(Attend
     if (tile == 0 && split == 0) refuse<IO>(a, s, l, h);
     return;
   }
-  const int f0 = tile * kRowsFew, rows = min(s.n * a.group - f0, kRowsFew);
+  const int f0 = tile * R, rows = min(s.n * a.group - f0, R);
   if (rows <= 0) return;
-  const Row r = row_of(a, s, h, f0 + c16);
+  const Row r = row_of(a, s, h, f0 + (c16 & (R - 1)));
   int most = r.sees, least = r.fine ? r.sees : INT_MAX;
+  if constexpr (R > 1) {
 #pragma unroll
-  for (int o = 8; o >= 1; o >>= 1) {
-    most = max(most, __shfl_xor(most, o, 64));
-    least = min(least, __shfl_xor(least, o, 64));
+    for (int o = R / 2; o >= 1; o >>= 1) {
+      most = max(most, __shfl_xor(most, o, 64));
+      least = min(least, __shfl_xor(least, o, 64));
+    }
   }
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
@@ -151,153 +200,226 @@ __global__ __launch_bounds__(W * 64, PARTS == 2 ? 4 : 3) void attend4_few(Attend
   const uint8_t* scales = a.cache4.scales + region * kScales4;
   const uint32_t koff = c16 * (kDim / 2) + g * 8, voff = c16 * 64 + g * 16;
 
-  float m = lowest(), lsum = 0.0f;
+  float m[kRows], lsum[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    m[i] = lowest();
+    lsum[i] = 0.0f;
+  }
   f32x4 O[4] = {};
 
-  // One page: its keys (token 16 j + c16, dimensions 16 g .. +15, and the four tokens'
-  // scales) and values (dimensions 4 c16 .. +3 of tokens 16 i + 4 g + r: i = 2 n and 2 n + 1
-  // in vw[n], and the scales of these sixteen).
-  // One that is not there is page 0 with scales of NaN for the keys and 2^-127 for
-  // the values, so that only rows that see it get NaN, whatever page 0 holds.
+  // One page: its keys (token 16 i + c16, dimensions 16 g .. +15), values (dimensions 4 c16
+  // .. +3 of tokens 16 i + 4 g + j: i = 2 n and 2 n + 1 in vw[n]) and the scales of the lane's
+  // tokens: 16 i + c16 for all i, the values' in byte c16 % 4 of four words; or 16 g + c16.
+  // A page that is not there is page 0 with keys that are no numbers, so that only
+  // rows that see it get NaN, whatever page 0 holds.
   u32x2 kw[4];
-  u32x4 vw[2], vs;
-  uint32_t ks;
+  u32x4 vw[2];
+  uint32_t ks, vs[kTokens];
   auto page_of = [&](int i, bool& bad) {
     const int page = __builtin_amdgcn_readlane(entries, i);
     bad = page < 0 || page >= a.cache4.pages;
     return bad ? 0 : page;
   };
-  auto load_keys = [&](int page, bool bad) {
+  auto load_keys = [&](int page) {
     const uint8_t* p = kplane + (int64_t)page * kPlane4;
 #pragma unroll
     for (int j = 0; j < 4; ++j) kw[j] = *reinterpret_cast<const u32x2*>(p + koff + j * 16 * (kDim / 2));
-    ks = *reinterpret_cast<const uint32_t*>(scales + (int64_t)page * kScales4 + c16 * 4);
-    if (bad) ks = 0xFFFFFFFFu;
   };
-  auto load_values = [&](int page, bool bad) {
+  auto load_scales = [&](int page, bool bad) {
+    const uint8_t* p = scales + (int64_t)page * kScales4;
+    if constexpr (kPacked) {
+      ks = p[c16 * 4 + g];
+      vs[0] = p[kPage + (c16 >> 2) * 16 + g * 4 + (c16 & 3)];
+    } else {
+      ks = *reinterpret_cast<const uint32_t*>(p + c16 * 4);
+      const u32x4 w = *reinterpret_cast<const u32x4*>(p + kPage + (c16 >> 2) * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vs[i] = w[i];
+    }
+    if (bad) {
+      ks = 0xFFFFFFFFu;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i) vs[i] = 0x7F7F7F7Fu;
+    }
+  };
+  auto load_values = [&](int page) {
     const uint8_t* p = vplane + (int64_t)page * kPlane4;
 #pragma unroll
     for (int n = 0; n < 2; ++n) vw[n] = *reinterpret_cast<const u32x4*>(p + voff + n * 1024);
-    vs = *reinterpret_cast<const u32x4*>(scales + (int64_t)page * kScales4 + kPage + g * 16);
-    if (bad) vs = u32x4{};
   };
   // The wave's first keys, before the query is worked on.
   bool bad = false;
   auto start = [&](int first) {
     if (a.nsplit > 1 || first > begin) entries = lane < (end - first + W - 1) / W ? table[first + lane * W] : 0;
     const int page = page_of(0, bad);
-    load_keys(page, bad);
+    load_keys(page);
+    load_scales(page, bad);
     return page;
   };
   int page = begin < end ? start(begin) : 0;
 
-  // q': lane (g, column) has dimensions 16 g .. 16 g + 15 of its row
-  bf16x8 q[PARTS][2];
+  // q': lane (g, row) has dimensions 16 g .. 16 g + 15 of its row, over a power of two; what
+  // its scores are multiplied by, and how many tokens it sees, go to the lanes that have them
+  f16x8 qh[2], ql[2];
+  float by[kRows];
+  int sees[kRows];
   {
     float x[16];
     rotate_query(query, 16 * g, x);
-    query_parts<16, 16, PARTS>(x, q);
+    hadamard_query<16, 16>(x);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, abs_bits(x[i]));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+    const int e = row_exponent<kBF16, kNone>(top);
+    split8<1>(x, e, qh[0], ql[0]);
+    split8<1>(x + 8, e, qh[1], ql[1]);
+    const float mine = a.scale2 * pow2(max(e, -126));
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      by[i] = R == 1 ? mine : __shfl(mine, kPacked ? i : 4 * g + i, 64);
+      sees[i] = R == 1 ? r.sees : __shfl(r.sees, kPacked ? i : 4 * g + i, 64);
+    }
   }
+
+  // Where a lane leaves its weights, and where it finds the row's that it takes to the second product: token 16 i + 4 g' + j
+  // is the 32 (j / 2) + 8 g' + 4 (j % 2) + i th.
+  uint8_t* weights = reinterpret_cast<uint8_t*>(s_o + wave * kRoom);
+  uint8_t* put = weights + (kPacked ? 0 : 4 * g * kWeights) + ((c16 & 2) * 16 + (c16 >> 2) * 8 + (c16 & 1) * 4 + (kPacked ? g : 0)) * 2;
+  const uint8_t* get = weights + (c16 & (R - 1)) * kWeights + g * 16;
 
   auto attend = [&](int tl, int next, bool next_bad) {   // next: the page after this one, or -1
     f32x4 S[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float by = scale_in(ks, i);
-      const bf16x8 k0 = values_bf16(kw[i][0], by), k1 = values_bf16(kw[i][1], by);
+      const f16x8 k0 = codes_f16(kw[i][0]), k1 = codes_f16(kw[i][1]);
       f32x4 z = {};
-#pragma unroll
-      for (int n = PARTS - 1; n >= 0; --n) {
-        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[n][0], z, 0, 0, 0);
-        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[n][1], z, 0, 0, 0);
-      }
-      S[i] = z;
+      z = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql[0], k0, z, 0, 0, 0);
+      z = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql[1], k1, z, 0, 0, 0);
+      z = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh[0], k0, z, 0, 0, 0);
+      S[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh[1], k1, z, 0, 0, 0);
     }
     // (the registers that this page's keys leave take the next one's)
-    if (next >= 0) load_keys(next, next_bad);
-    const int tok0 = tl * kPage + 4 * g;
-    if ((tl + 1) * kPage > least) {
+    if (next >= 0) load_keys(next);
+    float x[kTokens][kRows], over[kTokens];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kTokens; ++i) {
+      const uint32_t kb = kPacked ? ks : __builtin_amdgcn_ubfe(ks, 8 * i, 8), vb = kPacked ? vs[0] & 0xFF : __builtin_amdgcn_ubfe(vs[i], 8 * (c16 & 3), 8);
+      const float key = __uint_as_float(kb << 23);
+      // (zero times a scale of infinity is no number)
+      const float value = fmaf(key, 0.0f, (float)vb - 127.0f);
+      over[i] = __uint_as_float((254 - vb) << 23);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (tok0 + 16 * i + j >= r.sees) S[i][j] = -INFINITY;
-        // (what lies behind the sequence may be anything: codes are finite, and so are these scales)
-        vs[i] &= below(tok0 + 16 * i, s.len);
+      for (int j = 0; j < kRows; ++j) {
+        const float score = !kPacked ? S[i][j] : g == 0 ? S[0][j] : g == 1 ? S[1][j] : g == 2 ? S[2][j] : S[3][j];
+        x[i][j] = fmaf(score * by[j], key, value);
       }
     }
-    float c = a.scale2, top = S[0][0];
+    if ((tl + 1) * kPage > least) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < kTokens; ++i) {
+        const int tok = tl * kPage + (kPacked ? lane : 16 * i + c16);
+        // (what lies behind the sequence may be anything)
+        if (tok >= s.len) over[i] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) top = fmaxf(top, S[i][j]);
-    top = max_across16(max_across32(top)) * c;
-    if (rounds_first(top)) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) S[i] *= c;
-      c = 1.0f;
+        for (int j = 0; j < kRows; ++j)
+          if (tok >= sees[j]) x[i][j] = -INFINITY;
+      }
     }
-    if (__any(top - m > kRaise)) {
-      const float next = top - m > kRaise ? top : m;
-      const float f = __builtin_amdgcn_exp2f(m - next);
-      m = next;
-      lsum *= f;
+    if (next >= 0) load_scales(next, next_bad);
+    float rise = -INFINITY, top[kRows];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) O[i] *= f;
+    for (int j = 0; j < kRows; ++j) {
+      top[j] = x[0][j];
+#pragma unroll
+      for (int i = 1; i < kTokens; ++i) top[j] = fmaxf(top[j], x[i][j]);
+      rise = fmaxf(rise, top[j] - m[j]);
+    }
+    if (__any(rise > kRaise)) {
+#pragma unroll
+      for (int j = 0; j < kRows; ++j) {
+#pragma unroll
+        for (int o = kPacked ? 32 : 8; o >= 1; o >>= 1) top[j] = fmaxf(top[j], __shfl_xor(top[j], o, 64));
+        const float to = top[j] - m[j] > kRaise ? top[j] - kTop : m[j];
+        const float f = __builtin_amdgcn_exp2f(m[j] - to);
+        m[j] = to;
+        lsum[j] *= f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) O[d][j] *= f;
+      }
     }
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {              // tokens 32 n .. 32 n + 31
-      u32x4 pw[PARTS];
+    for (int j = 0; j < kRows; ++j) {
+      float p[kTokens];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < kTokens; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(x[i][j] - m[j]);
+        lsum[j] = fmaf(p[i], over[i], lsum[j]);
+      }
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(S[2 * n + i][j], c, -m)), p1 = __builtin_amdgcn_exp2f(fmaf(S[2 * n + i][j + 1], c, -m));
-          lsum += p0 + p1;
-          uint32_t w[PARTS];
-          split2<PARTS>(p0, p1, w);
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p) pw[p][2 * i + j / 2] = w[p];
+      for (int n = 0; n < WPARTS; ++n) {
+        uint8_t* to = put + (n * R + j) * kWeights;
+        if constexpr (kPacked) {
+          *reinterpret_cast<_Float16*>(to) = (_Float16)p[0];
+        } else {
+          *reinterpret_cast<f16x4*>(to) = f16x4{(_Float16)p[0], (_Float16)p[1], (_Float16)p[2], (_Float16)p[3]};
         }
+        if (n + 1 < WPARTS) {
+#pragma unroll
+          for (int i = 0; i < kTokens; ++i) p[i] -= (float)(_Float16)p[i];
+        }
+      }
+    }
+    // (LDS works off a wave's accesses in order)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      f16x8 P[WPARTS];
+#pragma unroll
+      for (int w = 0; w < WPARTS; ++w) P[w] = *reinterpret_cast<const f16x8*>(get + w * R * kWeights + n * 64);
       u32x4 v[4];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t out[4];
-        values_pairs(vw[n][w], scale_in(vs[2 * n + w / 2], 2 * (w & 1)), scale_in(vs[2 * n + w / 2], 2 * (w & 1) + 1), out);
-#pragma unroll
-        for (int d = 0; d < 4; ++d) v[d][w] = out[d];
+      for (int i = 0; i < 2; ++i) {            // tokens of 16 (2 i) and 16 (2 i + 1), two of each
+        codes_pairs(vw[i][n], vw[i][n + 2], v, i);
       }
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p)
-          O[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[d]), __builtin_bit_cast(bf16x8, pw[p]), O[d], 0, 0, 0);
+        for (int w = WPARTS - 1; w >= 0; --w)
+          O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(P[w], __builtin_bit_cast(f16x8, v[d]), O[d], 0, 0, 0);
     }
-    if (next >= 0) load_values(next, next_bad);
+    if (next >= 0) load_values(next);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   };
   for (int first = begin; first < end; first += 64 * W) {
     const int n = min(64, (end - first + W - 1) / W);
     if (first > begin) page = start(first);
-    load_values(page, bad);
+    load_values(page);
     for (int i = 0; i < n; ++i) {
       bad = false;
       page = i + 1 < n ? page_of(i + 1, bad) : -1;
       attend(first + i * W, page, bad);
     }
   }
-  lsum += __shfl_xor(lsum, 16, 64);
-  lsum += __shfl_xor(lsum, 32, 64);
-  if (g == 0) {
-    s_m[wave][c16] = m;
-    s_l[wave][c16] = lsum;
-  }
-  // O[d][j] is dimension 16 g + 4 j + d of row c16
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    *reinterpret_cast<f32x4*>(s_o + (wave * kRowsFew + c16) * kStride + 16 * g + 4 * j) = f32x4{O[0][j], O[1][j], O[2][j], O[3][j]};
+  for (int j = 0; j < kRows; ++j) {
+#pragma unroll
+    for (int o = kPacked ? 32 : 8; o >= 1; o >>= 1) lsum[j] += __shfl_xor(lsum[j], o, 64);
+    if ((kPacked ? lane : c16) == 0) {
+      s_m[wave][kPacked ? j : 4 * g + j] = m[j];
+      s_l[wave][kPacked ? j : 4 * g + j] = lsum[j];
+    }
+    // O[d][j] is dimension 4 c16 + d of row 4 g + j, or of row j in every group
+    if (!kPacked || g == 0)
+      *reinterpret_cast<f32x4*>(s_o + wave * kRoom + (kPacked ? j : 4 * g + j) * kStride + 4 * c16) = f32x4{O[0][j], O[1][j], O[2][j], O[3][j]};
+  }
   __syncthreads();
 
-  float* part = parts > 1 ? part_of(a, unit, split, kRowsFew) : nullptr;
+  float* part = parts > 1 ? part_of(a, unit, split, R) : nullptr;
   for (int e = t; e < rows * (kDim / 4); e += W * 64) {
     const int q = e / (kDim / 4), d = e % (kDim / 4) * 4;
     float M = lowest(), L = 0.0f;
@@ -308,7 +430,7 @@ __global__ __launch_bounds__(W * 64, PARTS == 2 ? 4 : 3) void attend4_few(Attend
     for (int w = 0; w < W; ++w) {
       const float f = __builtin_amdgcn_exp2f(s_m[w][q] - M);
       L += s_l[w][q] * f;
-      o += *reinterpret_cast<const f32x4*>(s_o + (w * kRowsFew + q) * kStride + d) * f;
+      o += *reinterpret_cast<const f32x4*>(s_o + w * kRoom + q * kStride + d) * f;
     }
     if (parts > 1) {
       store_part(part + q * kPartRow + d, o);
@@ -321,7 +443,7 @@ __global__ __launch_bounds__(W * 64, PARTS == 2 ? 4 : 3) void attend4_few(Attend
     }
   }
   if (parts == 1) return;
-  join_parts<IO, kRowsFew, true>(a, s, l, h, f0, rows, unit, parts, s_o, &s_last);
+  join_parts<IO, R, true>(a, s, l, h, f0, rows, unit, parts, s_o, &s_last);
 }
 
 // ------------------------------------------------------------ many rows
@@ -458,7 +580,8 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
     Query<IO, 32, ROPE> query;
     load_query(a, r, l, 32 * half, query);
     rotate_query(query, 32 * half, x);
-    query_parts<32, 32, QPARTS>(x, q);
+    hadamard_query<32, 32>(x);
+    query_parts<32, QPARTS>(x, q);
   }
 
   float m = lowest(), lsum = 0.0f;
@@ -619,7 +742,8 @@ AttendPlan plan_attend4(int64_t units0, int64_t rows, int max_len) {
   p.few = rows <= 64;
   // Blocks of 128 rows where these fill the chip three times, else of 64.
   p.groups = units0 * ((rows + 4 * kRowsMany - 1) / (4 * kRowsMany)) < 768 ? 2 : 1;
-  const int per = p.few ? kRowsFew : 4 * kRowsMany / p.groups;
+  const int per = !p.few ? 4 * kRowsMany / p.groups : rows <= 4 ? (int)(rows == 1 ? 1 : 4) : 16;
+  p.rows = per;
   p.tiles = (int)((rows + per - 1) / per);
   p.units = units0 * p.tiles;
   p.nsplit = 1;
@@ -635,11 +759,22 @@ AttendPlan plan_attend4(int64_t units0, int64_t rows, int max_len) {
   if (pages <= 8 && p.units >= 2048) p.waves = 1;
   const int64_t split = std::min<int64_t>(std::min<int64_t>(256 / p.units, pages / 16), kMaxSplit);
   if (p.waves == 8 && split > 1 && pages * (split - 1) >= 20 * split) p.nsplit = (int)split;
-  if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * kRowsFew * kPartRow * sizeof(float);
+  if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * per * kPartRow * sizeof(float);
   return p;
 }
 
 namespace {
+
+template <int IO, int WPARTS, int ROPE, int R>
+void few(const Attend4Args& a, const AttendPlan& p, const AttendGrid& g, dim3 grid, hipStream_t st) {
+  constexpr int kParts = WPARTS > 2 ? 2 : 1;
+  if (p.waves == 1)
+    hipLaunchKernelGGL((attend4_few<IO, kParts, ROPE, 1, R>), grid, dim3(64), 0, st, a, g);
+  else if (p.waves == 8)
+    hipLaunchKernelGGL((attend4_few<IO, kParts, ROPE, 8, R>), grid, dim3(512), 0, st, a, g);
+  else
+    hipLaunchKernelGGL((attend4_few<IO, kParts, ROPE, 4, R>), grid, dim3(256), 0, st, a, g);
+}
 
 template <int IO, int QPARTS, int WPARTS, int ROPE>
 hipError_t launch(const Attend4Args& a, const AttendPlan& p, hipStream_t st) {
@@ -655,12 +790,12 @@ hipError_t launch(const Attend4Args& a, const AttendPlan& p, hipStream_t st) {
     hipLaunchKernelGGL((attend4_many<IO, QPARTS, WPARTS, ROPE, 1>), grid, block, 0, st, a, g);
   else if (!p.few)
     hipLaunchKernelGGL((attend4_many<IO, QPARTS, WPARTS, ROPE, 2>), grid, block, 0, st, a, g);
-  else if (p.waves == 1)
-    hipLaunchKernelGGL((attend4_few<IO, QPARTS, ROPE, 1>), grid, block, 0, st, a, g);
-  else if (p.waves == 8)
-    hipLaunchKernelGGL((attend4_few<IO, QPARTS, ROPE, 8>), grid, block, 0, st, a, g);
+  else if (p.rows == 1)
+    few<IO, WPARTS, ROPE, 1>(a, p, g, grid, st);
+  else if (p.rows == 4)
+    few<IO, WPARTS, ROPE, 4>(a, p, g, grid, st);
   else
-    hipLaunchKernelGGL((attend4_few<IO, QPARTS, ROPE, 4>), grid, block, 0, st, a, g);
+    few<IO, WPARTS, ROPE, 16>(a, p, g, grid, st);
   return hipGetLastError();
 }
 
