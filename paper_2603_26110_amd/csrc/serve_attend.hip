@@ -16,6 +16,7 @@
 // The cache is in the Hadamard basis. A query row is brought there once (64 entries,
 // six butterflies, mostly within a lane), its result back once.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_rows.hpp"
 #include "serve_device.hpp"
@@ -211,11 +212,11 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
   // One page: its keys (token 16 i + c16, dimensions 16 g .. +15), values (dimensions 4 c16
   // .. +3 of tokens 16 i + 4 g + j: i = 2 n and 2 n + 1 in vw[n]) and the scales of the lane's
   // tokens: 16 i + c16 for all i, the values' in byte c16 % 4 of four words; or 16 g + c16.
-  // A page that is not there is page 0 with keys that are no numbers, so that only
+  // A page that is not there is page 0 with keys that are no numbers and scales of 2^-127 for the values, so that only
   // rows that see it get NaN, whatever page 0 holds.
   u32x2 kw[4];
   u32x4 vw[2];
-  uint32_t ks, vs[kTokens];
+  uint32_t ks, vs[kTokens], lost = 0;
   auto page_of = [&](int i, bool& bad) {
     const int page = __builtin_amdgcn_readlane(entries, i);
     bad = page < 0 || page >= a.cache4.pages;
@@ -237,11 +238,7 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
 #pragma unroll
       for (int i = 0; i < 4; ++i) vs[i] = w[i];
     }
-    if (bad) {
-      ks = 0xFFFFFFFFu;
-#pragma unroll
-      for (int i = 0; i < kTokens; ++i) vs[i] = 0x7F7F7F7Fu;
-    }
+    lost = bad ? 0xFFFFFFFFu : 0u;             // (what is loaded changes where it is used, or this would wait for it)
   };
   auto load_values = [&](int page) {
     const uint8_t* p = vplane + (int64_t)page * kPlane4;
@@ -276,6 +273,10 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
     const int e = row_exponent<kBF16, kNone>(top);
     split8<1>(x, e, qh[0], ql[0]);
     split8<1>(x + 8, e, qh[1], ql[1]);
+    if constexpr (R == 1) {                    // (both parts as rows of their own)
+      qh[0] = c16 & 1 ? ql[0] : qh[0];
+      qh[1] = c16 & 1 ? ql[1] : qh[1];
+    }
     const float mine = a.scale2 * pow2(max(e, -126));
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
@@ -290,30 +291,37 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
   uint8_t* put = weights + (kPacked ? 0 : 4 * g * kWeights) + ((c16 & 2) * 16 + (c16 >> 2) * 8 + (c16 & 1) * 4 + (kPacked ? g : 0)) * 2;
   const uint8_t* get = weights + (c16 & (R - 1)) * kWeights + g * 16;
 
-  auto attend = [&](int tl, int next, bool next_bad) {   // next: the page after this one, or -1
+  // more: whether `next` takes this page's place. (Known to the compiler, which then knows what is on its way, too, and
+  // waits for no more than it needs.)
+  auto attend = [&](auto more, int tl, int next, bool next_bad) {
+    constexpr bool kMore = decltype(more)::value;
     f32x4 S[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const f16x8 k0 = codes_f16(kw[i][0]), k1 = codes_f16(kw[i][1]);
       f32x4 z = {};
-      z = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql[0], k0, z, 0, 0, 0);
-      z = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql[1], k1, z, 0, 0, 0);
+      if constexpr (R > 1) {
+        z = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql[0], k0, z, 0, 0, 0);
+        z = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql[1], k1, z, 0, 0, 0);
+      }
       z = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh[0], k0, z, 0, 0, 0);
       S[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh[1], k1, z, 0, 0, 0);
     }
     // (the registers that this page's keys leave take the next one's)
-    if (next >= 0) load_keys(next);
+    if (kMore) load_keys(next);
     float x[kTokens][kRows], over[kTokens];
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) {
-      const uint32_t kb = kPacked ? ks : __builtin_amdgcn_ubfe(ks, 8 * i, 8), vb = kPacked ? vs[0] & 0xFF : __builtin_amdgcn_ubfe(vs[i], 8 * (c16 & 3), 8);
+      const uint32_t kb = kPacked ? (ks | lost) & 0xFF : __builtin_amdgcn_ubfe(ks | lost, 8 * i, 8);
+      const uint32_t vb = kPacked ? vs[0] & ~lost : __builtin_amdgcn_ubfe(vs[i] & ~lost, 8 * (c16 & 3), 8);
       const float key = __uint_as_float(kb << 23);
       // (zero times a scale of infinity is no number)
       const float value = fmaf(key, 0.0f, (float)vb - 127.0f);
       over[i] = __uint_as_float((254 - vb) << 23);
 #pragma unroll
       for (int j = 0; j < kRows; ++j) {
-        const float score = !kPacked ? S[i][j] : g == 0 ? S[0][j] : g == 1 ? S[1][j] : g == 2 ? S[2][j] : S[3][j];
+        const f32x4 part = !kPacked ? S[i] : g == 0 ? S[0] : g == 1 ? S[1] : g == 2 ? S[2] : S[3];
+        const float score = R == 1 ? part[0] + part[1] : part[j];
         x[i][j] = fmaf(score * by[j], key, value);
       }
     }
@@ -328,7 +336,7 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
           if (tok >= sees[j]) x[i][j] = -INFINITY;
       }
     }
-    if (next >= 0) load_scales(next, next_bad);
+    if (kMore) load_scales(next, next_bad);
     float rise = -INFINITY, top[kRows];
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
@@ -391,7 +399,7 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
         for (int w = WPARTS - 1; w >= 0; --w)
           O[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(P[w], __builtin_bit_cast(f16x8, v[d]), O[d], 0, 0, 0);
     }
-    if (next >= 0) load_values(next);
+    if (kMore) load_values(next);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   };
@@ -399,11 +407,11 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
     const int n = min(64, (end - first + W - 1) / W);
     if (first > begin) page = start(first);
     load_values(page);
-    for (int i = 0; i < n; ++i) {
-      bad = false;
-      page = i + 1 < n ? page_of(i + 1, bad) : -1;
-      attend(first + i * W, page, bad);
+    for (int i = 0; i + 1 < n; ++i) {
+      page = page_of(i + 1, bad);
+      attend(std::true_type(), first + i * W, page, bad);
     }
+    attend(std::false_type(), first + (n - 1) * W, 0, false);
   }
 #pragma unroll
   for (int j = 0; j < kRows; ++j) {
@@ -755,7 +763,7 @@ AttendPlan plan_attend4(int64_t units0, int64_t rows, int max_len) {
     if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * (2 * kRowsMany) * kPartRow * sizeof(float);
     return p;
   }
-  if ((p.units <= 256 && pages >= 16) || pages >= 64) p.waves = 8;
+  if ((p.units <= 256 && pages >= 16) ) p.waves = 8;
   if (pages <= 8 && p.units >= 2048) p.waves = 1;
   const int64_t split = std::min<int64_t>(std::min<int64_t>(256 / p.units, pages / 16), kMaxSplit);
   if (p.waves == 8 && split > 1 && pages * (split - 1) >= 20 * split) p.nsplit = (int)split;
