@@ -225,7 +225,7 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
   auto load_keys = [&](int page) {
     const uint8_t* p = kplane + (int64_t)page * kPlane4;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) kw[j] = *reinterpret_cast<const u32x2*>(p + koff + j * 16 * (kDim / 2));
+    for (int j = 0; j < 4; ++j) kw[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p + koff + j * 16 * (kDim / 2)));
   };
   auto load_scales = [&](int page, bool bad) {
     const uint8_t* p = scales + (int64_t)page * kScales4;
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
   auto load_values = [&](int page) {
     const uint8_t* p = vplane + (int64_t)page * kPlane4;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) vw[n] = *reinterpret_cast<const u32x4*>(p + voff + n * 1024);
+    for (int n = 0; n < 2; ++n) vw[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + voff + n * 1024));
   };
   // The wave's first keys, before the query is worked on.
   bool bad = false;
@@ -763,10 +763,16 @@ AttendPlan plan_attend4(int64_t units0, int64_t rows, int max_len) {
     if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * (2 * kRowsMany) * kPartRow * sizeof(float);
     return p;
   }
-  if ((p.units <= 256 && pages >= 16) ) p.waves = 8;
+  if (p.units <= 256 && pages >= 16) p.waves = 8;
   if (pages <= 8 && p.units >= 2048) p.waves = 1;
-  const int64_t split = std::min<int64_t>(std::min<int64_t>(256 / p.units, pages / 16), kMaxSplit);
-  if (p.waves == 8 && split > 1 && pages * (split - 1) >= 20 * split) p.nsplit = (int)split;
+  // A unit's pages are shared by blocks where these find free compute units and each wave is
+  // spared pages enough for the storing and joining. 65 to 128 units of long sequences take twice as
+  // many blocks of half the size (128 units of 128 pages and five rows 29.2 -> 25.5 us, 72 23.2 -> 21.1; 192 of 64
+  // would go 20.5 -> 25.6, 20 of 250 pages 17.8 -> 20.8).
+  const bool halves = p.units > 64 && p.units <= 128 && pages >= 64;
+  if (halves) p.waves = 4;
+  const int64_t split = std::min<int64_t>(std::min<int64_t>((halves ? 512 : 256) / p.units, pages / 16), kMaxSplit);
+  if ((p.waves == 8 || halves) && split > 1 && pages * (split - 1) >= 20 * split) p.nsplit = (int)split;
   if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * per * kPartRow * sizeof(float);
   return p;
 }
