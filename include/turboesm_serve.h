@@ -105,7 +105,7 @@ TQ_API tq_status tqs_norm_rope(const tqp_params* params, const tqp_rows* q, cons
  * which of both (other tokens are not touched).
  *
  *   k, v   device rows [nlayers][rows][kv_heads][64] of io_dtype.
- *          nlayers * kv_heads * ceil(rows / 32) is less than 2^24.
+ *          nlayers * kv_heads * ceil(rows / 64) is less than 2^24.
  *   slots  device int64 [rows];  pos device int32 [rows] (unused and may be
  *          NULL without rope_cs).
  */
@@ -119,7 +119,7 @@ TQ_API tq_status tqs_append(const tqp_params* params, const tqs_cache* cache, co
  * is no number gives NaN for the key, zeros for the value. A row with a slot
  * outside [0, 64*pages) gets NaN for both.
  *   k, v   device [nlayers][rows][kv_heads][64], contiguous, 16-byte aligned.
- *          nlayers * kv_heads * ceil(rows / 32) is less than 2^24.
+ *          nlayers * kv_heads * ceil(rows / 64) is less than 2^24.
  */
 TQ_API tq_status tqs_read(const tqp_params* params, const tqs_cache* cache, const int64_t* slots, int32_t rows,
                           int32_t layer0, int32_t nlayers, void* k, void* v, void* stream);

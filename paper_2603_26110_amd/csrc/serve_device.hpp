@@ -37,7 +37,7 @@ __device__ __forceinline__ uint32_t codes8(const float* x, float by) {
 }
 
 // Eight codes times a scale (its exponent's bits; NaN where they are all set).
-__device__ __forceinline__ void values8(uint32_t w, float by, float (&x)[8]) {
+__device__ __forceinline__ void values8(uint32_t w, float by, float* x) {
   const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 1);
   const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 3);
   x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
@@ -46,29 +46,31 @@ __device__ __forceinline__ void values8(uint32_t w, float by, float (&x)[8]) {
 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float((byte & 0xFFu) << 23); }
 
-// ------------------------------------------------- vectors of 64 in eight lanes
-// What the lane 1, 2 or 4 away (in its number's bits) holds.
+// ------------------------------------------------- vectors of 64 in four lanes
+// Lane j of four (its number's last two bits) has entries 16 j .. 16 j + 15, or (SPLIT) 8 j ..
+// 8 j + 7 and those 32 further: so that the pairs of either kind are whole in a lane, and
+// everything moves in 16 bytes.
+template <bool SPLIT>
+__device__ __forceinline__ int run_of(int j, int half) { return SPLIT ? 8 * j + 32 * half : 16 * j + 8 * half; }
+
+// What the lane 1 or 2 away (in its number's bits) holds.
 template <int WITH>
 __device__ __forceinline__ float across(float x) {
-  const int v = __float_as_int(x);
-  if constexpr (WITH == 1) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true));   // (within each four)
-  if constexpr (WITH == 2) return __int_as_float(__builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true));
-  // lanes 0-3 and 8-11 of a row take from four above, the others from four below
-  const int up = __builtin_amdgcn_update_dpp(v, v, 0x104, 0xF, 0x5, false);
-  return __int_as_float(__builtin_amdgcn_update_dpp(up, v, 0x114, 0xF, 0xA, false));
+  static_assert(WITH == 1 || WITH == 2, "within four lanes");
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), WITH == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true));
 }
 
 template <int WITH>
-__device__ __forceinline__ void butterfly(float (&x)[8], int j) {
+__device__ __forceinline__ void butterfly(float (&x)[16], int j) {
   const float sign = j & WITH ? -1.0f : 1.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = fmaf(sign, x[i], across<WITH>(x[i]));   // (a sum or difference, rounded once)
+  for (int i = 0; i < 16; ++i) x[i] = fmaf(sign, x[i], across<WITH>(x[i]));   // (a sum or difference, rounded once)
 }
 
 template <int STEP>
-__device__ __forceinline__ void butterfly_within(float (&x)[8]) {
+__device__ __forceinline__ void butterfly_within(float (&x)[16]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 16; ++i)
     if (!(i & STEP)) {
       const float a = x[i], b = x[i + STEP];
       x[i] = a + b;
@@ -77,43 +79,34 @@ __device__ __forceinline__ void butterfly_within(float (&x)[8]) {
 }
 
 // A vector times the Hadamard matrix over 8, in the order of the entries' distance
-// (1, 2, .. 32) that the codes' definition asks for. Lane j of eight has entries 8 j
-// .. 8 j + 7, or (SPLIT) 4 j .. 4 j + 3 and those 32 further.
+// (1, 2, .. 32) that the codes' definition asks for.
 template <bool SPLIT>
-__device__ __forceinline__ void hadamard8(float (&x)[8], int j) {
+__device__ __forceinline__ void hadamard16(float (&x)[16], int j) {
   butterfly_within<1>(x);
   butterfly_within<2>(x);
-  if (!SPLIT) butterfly_within<4>(x);
+  butterfly_within<4>(x);
+  if (!SPLIT) butterfly_within<8>(x);
   butterfly<1>(x, j);
   butterfly<2>(x, j);
-  butterfly<4>(x, j);
-  if (SPLIT) butterfly_within<4>(x);
+  if (SPLIT) butterfly_within<8>(x);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] *= 0.125f;
+  for (int i = 0; i < 16; ++i) x[i] *= 0.125f;
 }
 
-__device__ __forceinline__ uint32_t max_of_eight(uint32_t m) {
+__device__ __forceinline__ uint32_t max_of_four(uint32_t m) {
   m = max(m, __float_as_uint(across<1>(__uint_as_float(m))));
-  m = max(m, __float_as_uint(across<2>(__uint_as_float(m))));
-  return max(m, __float_as_uint(across<4>(__uint_as_float(m))));
+  return max(m, __float_as_uint(across<2>(__uint_as_float(m))));
 }
 
-// Lane j's eight entries of a head, as binary32.
-template <int IO, bool SPLIT>
-__device__ __forceinline__ void load_eight(const void* base, int64_t head, int j, float (&x)[8]) {
-  if constexpr (SPLIT) {
-    float lo[4], hi[4];
-    load_elements<IO>(base, head + 4 * j, lo);
-    load_elements<IO>(base, head + 4 * j + 32, hi);
+// Eight elements, 16-byte aligned, as binary32.
+template <int IO>
+__device__ __forceinline__ void load_run(const void* base, int64_t at, float* x) {
+  if constexpr (IO == kF32) {
+    const f32x4* p = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(base) + at);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = lo[i];
-      x[4 + i] = hi[i];
-    }
-  } else if constexpr (IO == kF32) {
-    load_elements<IO>(base, head + 8 * j, x);
+    for (int i = 0; i < 8; ++i) x[i] = p[i >> 2][i & 3];
   } else {
-    const u32x4 v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(base) + head + 8 * j);
+    const u32x4 v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(base) + at);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t bits = (v[i >> 1] >> (16 * (i & 1))) & 0xFFFFu;
@@ -122,47 +115,57 @@ __device__ __forceinline__ void load_eight(const void* base, int64_t head, int j
   }
 }
 
-template <int IO, int N>
+template <int IO>
 __device__ __forceinline__ void store_run(void* base, int64_t at, const float* x) {
   if constexpr (IO == kF32) {
-    float* p = reinterpret_cast<float*>(base) + at;
-#pragma unroll
-    for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4*>(p + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+    f32x4* p = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(base) + at);
+    p[0] = f32x4{x[0], x[1], x[2], x[3]};
+    p[1] = f32x4{x[4], x[5], x[6], x[7]};
   } else {
-    uint32_t w[N / 2];
+    u32x4 w;
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       if constexpr (IO == kF16) w[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)x[2 * i], (_Float16)x[2 * i + 1]});
       else w[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
     }
-    uint16_t* p = reinterpret_cast<uint16_t*>(base) + at;
-    if constexpr (N == 8) *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
-    else *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
+    *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(base) + at) = w;
   }
 }
 
-// Lane j's eight entries to where load_eight takes them from.
+// Lane j's entries of a head.
 template <int IO, bool SPLIT>
-__device__ __forceinline__ void store_eight(void* base, int64_t head, int j, const float (&x)[8]) {
-  if constexpr (SPLIT) {
-    store_run<IO, 4>(base, head + 4 * j, x);
-    store_run<IO, 4>(base, head + 4 * j + 32, x + 4);
-  } else {
-    store_run<IO, 8>(base, head + 8 * j, x);
-  }
+__device__ __forceinline__ void load_lane(const void* base, int64_t head, int j, float (&x)[16]) {
+  load_run<IO>(base, head + run_of<SPLIT>(j, 0), x);
+  load_run<IO>(base, head + run_of<SPLIT>(j, 1), x + 8);
+}
+template <int IO, bool SPLIT>
+__device__ __forceinline__ void store_lane(void* base, int64_t head, int j, const float (&x)[16]) {
+  store_run<IO>(base, head + run_of<SPLIT>(j, 0), x);
+  store_run<IO>(base, head + run_of<SPLIT>(j, 1), x + 8);
 }
 
-// A lane's four pairs turned by (cos, sin) c: entries 2 i and 2 i + 1, or (SPLIT) i and
-// i + 4. Products and sums round on their own.
+// A lane's eight pairs (8 j .. 8 j + 7) turned by (cos, sin) c: entries 2 i and 2 i + 1, or
+// (SPLIT) i and i + 8. Products and sums round on their own.
 template <bool SPLIT>
-__device__ __forceinline__ void turn_eight(float (&x)[8], const float2 (&c)[4]) {
+__device__ __forceinline__ void turn_lane(float (&x)[16], const float2 (&c)[8]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 8; ++i) {
     float& a = x[SPLIT ? i : 2 * i];
-    float& b = x[SPLIT ? i + 4 : 2 * i + 1];
+    float& b = x[SPLIT ? i + 8 : 2 * i + 1];
     const float u = a * c[i].x - b * c[i].y, v = a * c[i].y + b * c[i].x;
     a = u;
     b = v;
+  }
+}
+
+// The angles of pairs 8 j .. 8 j + 7 at a position.
+__device__ __forceinline__ void load_angles(const float* cs, int64_t pos, int j, float2 (&c)[8]) {
+  const float4* p = reinterpret_cast<const float4*>(cs) + pos * (kDim / 4) + 4 * j;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 v = p[i];
+    c[2 * i] = make_float2(v.x, v.y);
+    c[2 * i + 1] = make_float2(v.z, v.w);
   }
 }
 

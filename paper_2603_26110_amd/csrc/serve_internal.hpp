@@ -54,7 +54,8 @@ struct VerifyArgs {
   const void* target;
   const void* draft;           // NULL: drafts are certain
   int64_t target_stride, draft_stride;
-  int io, vocab, rows, B, chunks;
+  int io, vocab, rows, B;
+  int entries, chunks;         // of a block; blocks of a sequence
   const int64_t* tokens;
   const int32_t* row0;
   const float* uniform;
@@ -72,7 +73,7 @@ hipError_t launch_append4(const StoreArgs& a, hipStream_t st);
 hipError_t launch_read4(const StoreArgs& a, hipStream_t st);
 AttendPlan plan_attend4(int64_t units0, int64_t rows_per_unit, int max_len);
 hipError_t launch_attend4(const Attend4Args& a, const AttendPlan& p, hipStream_t st);
-int verify_chunks(int vocab);                // blocks of a sequence
+int verify_entries(int vocab, int B);        // entries of a block
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);
 
 }  // namespace tqp

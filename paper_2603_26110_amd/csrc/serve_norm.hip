@@ -1,9 +1,10 @@
 // Norm of every query and key head and its rotation, in one pass (tqs_norm_rope).
 //
-// Eight lanes take a head: lane j has entries 8 j .. 8 j + 7 (or, in the half pairing,
-// 4 j .. 4 j + 3 and those 32 further), so that its pairs are whole, and the sum of
-// squares takes three steps across lanes. A wave has eight heads of one row, queries
-// and keys counted together: they share the row's angles.
+// Four lanes take a head, in 16-byte loads: lane j has entries 16 j .. 16 j + 15 (or, in the
+// half pairing, 8 j .. 8 j + 7 and those 32 further), so that its pairs are whole, and the
+// sum of squares takes two steps across lanes. A wave has sixteen heads of one row,
+// queries and keys counted together: the row's positions are scalars, its angles loaded
+// once for all of them.
 // Bound by memory: q and k are read and written once.
 #include "serve_device.hpp"
 
@@ -12,75 +13,79 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <int IO, int ROPE>
+template <int IO, int ROPE, bool ONE>
 __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormArgs a, uint32_t waves) {
   constexpr bool kSplit = ROPE == kHalf;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6));
   if (wave >= waves) return;
-  const int heads = a.heads + a.kv_heads, eights = (heads + 7) >> 3;
-  const int line = (int)(wave / (uint32_t)eights), l = line / a.rows, row = line - l * a.rows;
-  const int j = threadIdx.x & 7, head = (int)(wave - (uint32_t)line * eights) * 8 + ((threadIdx.x & 63) >> 3);
-  if (head >= heads) return;                 // (eight lanes at a time)
+  const int heads = a.heads + a.kv_heads, parts = (heads + 15) >> 4;
+  const int line = (int)(wave / (uint32_t)parts), l = line / a.rows, row = line - l * a.rows;
+  const int j = threadIdx.x & 3, head = (int)(wave - (uint32_t)line * parts) * 16 + ((threadIdx.x & 63) >> 2);
+  if (head >= heads) return;                 // (four lanes at a time)
   const bool key = head >= a.heads;
   const int h = key ? head - a.heads : head;
   const Rows& from = key ? a.k : a.q;
   const Rows& to = key ? a.k_out : a.q_out;
-  float x[8];
-  load_eight<IO, kSplit>(from.data, l * from.layer + row * from.row + h * from.head, j, x);
-  float2 c[4];
-  bool fine = true;
-  if constexpr (ROPE != kNone) {
+  float x[16];
+  load_lane<IO, kSplit>(from.data, l * from.layer + row * from.row + h * from.head, j, x);
+  float2 c[8];
+  bool fine = true;                          // (for the whole row)
+  if constexpr (ROPE != kNone && ONE) {
+    const int pos = a.pos[row];
+    fine = pos >= 0 && pos < a.rope_positions;
+    load_angles(a.cs, fine ? pos : 0, j, c);
+  } else if constexpr (ROPE != kNone) {
+    int at[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int pair = 4 * j + i;
-      int axis = 0;
-      for (int n = 1; n < a.axes; ++n) axis += pair >= a.first[n];
-      const int pos = a.pos[(int64_t)axis * a.rows + row];
+    for (int n = 0; n < kMaxAxes; ++n) {
+      if (n >= a.axes) break;
+      // (an axis without pairs does not count)
+      const int pos = a.pos[(int64_t)n * a.rows + row], end = n + 1 < a.axes ? a.first[n + 1] : kDim / 2;
       const bool in = pos >= 0 && pos < a.rope_positions;
-      fine = fine && in;
-      c[i] = reinterpret_cast<const float2*>(a.cs)[(int64_t)(in ? pos : 0) * (kDim / 2) + pair];
+      fine = fine && (in || end == a.first[n]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (n == 0 || 8 * j + i >= a.first[n]) at[i] = in ? pos : 0;
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = reinterpret_cast<const float2*>(a.cs)[(int64_t)at[i] * (kDim / 2) + 8 * j + i];
   }
   const float* weight = key ? a.k_weight : a.q_weight;
-  float w[8];
+  float w[16];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = 1.0f;
-  if (weight) load_eight<kF32, kSplit>(weight, (int64_t)l * kDim, j, w);
+  for (int i = 0; i < 16; ++i) w[i] = 1.0f;
+  if (weight) load_lane<kF32, kSplit>(weight, (int64_t)l * kDim, j, w);
   float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+  for (int i = 0; i < 16; ++i) sum = fmaf(x[i], x[i], sum);
   sum += across<1>(sum);
   sum += across<2>(sum);
-  sum += across<4>(sum);
   const float by = 1.0f / sqrtf(sum * (1.0f / kDim) + a.eps);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] *= by * w[i];
+  for (int i = 0; i < 16; ++i) x[i] *= by * w[i];
   if constexpr (ROPE != kNone) {
-    turn_eight<kSplit>(x, c);
-    // (all of a row: a lane that knows of a bad position tells the others)
-    float lost = fine ? 0.0f : 1.0f;
-    lost += across<1>(lost);
-    lost += across<2>(lost);
-    lost += across<4>(lost);
-    if (lost > 0.0f) {
+    turn_lane<kSplit>(x, c);
+    if (!fine) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = __builtin_nanf("");
+      for (int i = 0; i < 16; ++i) x[i] = __builtin_nanf("");
     }
   }
-  store_eight<IO, kSplit>(const_cast<void*>(to.data), l * to.layer + row * to.row + h * to.head, j, x);
+  store_lane<IO, kSplit>(const_cast<void*>(to.data), l * to.layer + row * to.row + h * to.head, j, x);
+}
+
+template <int IO, int ROPE, bool ONE>
+hipError_t launch(const NormArgs& a, hipStream_t st) {
+  const int64_t waves = (int64_t)a.nlayers * a.rows * ((a.heads + a.kv_heads + 15) / 16);
+  const dim3 grid((unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64))), block(kThreads);
+  hipLaunchKernelGGL((norm_rope_kernel<IO, ROPE, ONE>), grid, block, 0, st, a, (uint32_t)waves);
+  return hipGetLastError();
 }
 
 template <int IO>
 hipError_t launch(const NormArgs& a, hipStream_t st) {
-  const int64_t waves = (int64_t)a.nlayers * a.rows * ((a.heads + a.kv_heads + 7) / 8);
-  const dim3 grid((unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64))), block(kThreads);
-  if (!a.cs)
-    hipLaunchKernelGGL((norm_rope_kernel<IO, kNone>), grid, block, 0, st, a, (uint32_t)waves);
-  else if (a.rope_half)
-    hipLaunchKernelGGL((norm_rope_kernel<IO, kHalf>), grid, block, 0, st, a, (uint32_t)waves);
-  else
-    hipLaunchKernelGGL((norm_rope_kernel<IO, kPairs>), grid, block, 0, st, a, (uint32_t)waves);
-  return hipGetLastError();
+  if (!a.cs) return launch<IO, kNone, true>(a, st);
+  if (a.axes == 1) return a.rope_half ? launch<IO, kHalf, true>(a, st) : launch<IO, kPairs, true>(a, st);
+  return a.rope_half ? launch<IO, kHalf, false>(a, st) : launch<IO, kPairs, false>(a, st);
 }
 
 }  // namespace

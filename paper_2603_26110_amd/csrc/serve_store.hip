@@ -1,13 +1,12 @@
 // Keys and values into the 4-bit cache and out of it (tqs_append, tqs_read).
 //
 // A token's vector of one head is quantized on its own: no runs, no page whose scale
-// moves, and no byte that two tokens share. Eight lanes take the key and the value of a
-// (token, head): 16-byte loads, the rotation of whole pairs within a lane, three steps
-// of the Hadamard butterfly within a lane and three across eight (DPP), the largest
-// entry, and the conversion of the hardware, which rounds and saturates as the codes'
-// definition asks. In the half pairing a lane has entries 4 j .. and 32 + 4 j .. of a
-// key, so that its pairs are whole there, too. The eight groups of a wave have eight
-// rows of one head: a value plane keeps four tokens' bytes side by side.
+// moves, and no byte that two tokens share. Four lanes take the key and the value of a
+// (token, head): 16-byte loads, the rotation of whole pairs and four steps of the Hadamard
+// butterfly within a lane and two across four (DPP), the largest entry, and the conversion
+// of the hardware, which rounds and saturates as the codes' definition asks. The sixteen
+// groups of a wave have sixteen rows of one head: a value plane keeps the bytes of four
+// tokens side by side.
 //
 // The least traffic is 256 bytes of fp16 in and 66 out per token and head.
 #include <algorithm>
@@ -17,7 +16,7 @@
 namespace tqp {
 namespace {
 
-constexpr int kThreads = 256, kRows = kThreads / 8;   // of a block, of one (layer, head)
+constexpr int kThreads = 256, kRows = kThreads / 4;   // of a block, of one (layer, head)
 
 // A block's head and rows. Heads of the same rows follow each other.
 struct Part {
@@ -29,8 +28,8 @@ __device__ __forceinline__ Part part_of(const StoreArgs& a, int tiles) {
   Part p;
   p.h = id - rest * a.heads;
   p.l = rest / tiles;
-  p.row = (rest - p.l * tiles) * kRows + (threadIdx.x >> 3);
-  p.j = threadIdx.x & 7;
+  p.row = (rest - p.l * tiles) * kRows + (threadIdx.x >> 2);
+  p.j = threadIdx.x & 3;
   return p;
 }
 
@@ -38,48 +37,50 @@ template <int IO, int ROPE>
 __global__ __launch_bounds__(kThreads) void append4_kernel(StoreArgs a, int tiles) {
   constexpr bool kSplit = ROPE == kHalf;
   const Part p = part_of(a, tiles);
-  if (p.row >= a.rows) return;               // (eight lanes at a time)
+  if (p.row >= a.rows) return;               // (four lanes at a time)
   const int64_t slot = a.slots[p.row];
-  float k[8], v[8];
-  load_eight<IO, kSplit>(a.k.data, p.l * a.k.layer + p.row * a.k.row + p.h * a.k.head, p.j, k);
-  load_eight<IO, false>(a.v.data, p.l * a.v.layer + p.row * a.v.row + p.h * a.v.head, p.j, v);
+  float k[16], v[16];
+  load_lane<IO, kSplit>(a.k.data, p.l * a.k.layer + p.row * a.k.row + p.h * a.k.head, p.j, k);
+  load_lane<IO, false>(a.v.data, p.l * a.v.layer + p.row * a.v.row + p.h * a.v.head, p.j, v);
   bool there = slot >= 0 && slot < (int64_t)a.cache.pages * kPage;
   if constexpr (ROPE != kNone) {
     const int pos = a.pos[p.row];
     const bool fine = pos >= 0 && pos < a.rope_positions;
     there = there && fine;
-    const float4* cs = reinterpret_cast<const float4*>(a.cs) + (int64_t)(fine ? pos : 0) * (kDim / 4) + 2 * p.j;
-    const float4 c0 = cs[0], c1 = cs[1];
-    const float2 c[4] = {{c0.x, c0.y}, {c0.z, c0.w}, {c1.x, c1.y}, {c1.z, c1.w}};
-    turn_eight<kSplit>(k, c);
+    float2 c[8];
+    load_angles(a.cs, fine ? pos : 0, p.j, c);
+    turn_lane<kSplit>(k, c);
   }
   if (!there) return;
-  hadamard8<kSplit>(k, p.j);
-  hadamard8<false>(v, p.j);
+  hadamard16<kSplit>(k, p.j);
+  hadamard16<false>(v, p.j);
   uint32_t km = 0, vm = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 16; ++i) {
     km = max(km, abs_bits(k[i]));
     vm = max(vm, abs_bits(v[i]));
   }
-  km = max_of_eight(km);
-  vm = max_of_eight(vm);
+  km = max_of_four(km);
+  vm = max_of_four(vm);
   const bool bad = max(km, vm) >= kInfBits;
   const int ke = exponent4_of(km), ve = exponent4_of(vm);
-  const uint32_t kw = codes8(k, pow2(ke)), vw = bad ? 0 : codes8(v, pow2(ve));
 
   const int64_t region = ((int64_t)(a.layer0 + p.l) * a.heads + p.h) * a.cache.pages + (slot >> 6);
   const int t = (int)(slot & 63);
-  uint8_t* kp = a.cache.k + region * kPlane4 + key_at(t);
+  const uint32_t k0 = codes8(k, pow2(ke)), k1 = codes8(k + 8, pow2(ke));
+  uint32_t* kp = reinterpret_cast<uint32_t*>(a.cache.k + region * kPlane4 + key_at(t));
   if (kSplit) {
-    reinterpret_cast<uint16_t*>(kp)[p.j] = (uint16_t)kw;
-    reinterpret_cast<uint16_t*>(kp)[p.j + 8] = (uint16_t)(kw >> 16);
+    kp[p.j] = k0;
+    kp[p.j + 4] = k1;
   } else {
-    reinterpret_cast<uint32_t*>(kp)[p.j] = kw;
+    reinterpret_cast<u32x2*>(kp)[p.j] = u32x2{k0, k1};
   }
-  uint8_t* vp = a.cache.v + region * kPlane4 + value_at(t, 2 * p.j);
-  *reinterpret_cast<uint16_t*>(vp) = (uint16_t)vw;
-  *reinterpret_cast<uint16_t*>(vp + 64) = (uint16_t)(vw >> 16);
+  const uint32_t v0 = bad ? 0 : codes8(v, pow2(ve)), v1 = bad ? 0 : codes8(v + 8, pow2(ve));
+  uint8_t* vp = a.cache.v + region * kPlane4 + value_at(t, 4 * p.j);
+  *reinterpret_cast<uint16_t*>(vp) = (uint16_t)v0;
+  *reinterpret_cast<uint16_t*>(vp + 64) = (uint16_t)(v0 >> 16);
+  *reinterpret_cast<uint16_t*>(vp + 128) = (uint16_t)v1;
+  *reinterpret_cast<uint16_t*>(vp + 192) = (uint16_t)(v1 >> 16);
   if (p.j < 2) {
     const int at = p.j == 0 ? key_scale_at(t) : value_scale_at(t);
     a.cache.scales[region * kScales4 + at] = (uint8_t)(p.j == 0 ? (bad ? 255 : ke + 127) : (bad ? 127 : ve + 127));
@@ -92,25 +93,30 @@ __global__ __launch_bounds__(kThreads) void read4_kernel(StoreArgs a, int tiles)
   if (p.row >= a.rows) return;
   const int64_t slot = a.slots[p.row];
   const bool there = slot >= 0 && slot < (int64_t)a.cache.pages * kPage;
-  float k[8], v[8];
-  if (there) {                               // (eight lanes at a time)
+  float k[16], v[16];
+  if (there) {                               // (four lanes at a time)
     const int64_t region = ((int64_t)(a.layer0 + p.l) * a.heads + p.h) * a.cache.pages + (slot >> 6);
     const int t = (int)(slot & 63);
-    const uint32_t kw = reinterpret_cast<const uint32_t*>(a.cache.k + region * kPlane4 + key_at(t))[p.j];
-    const uint8_t* vp = a.cache.v + region * kPlane4 + value_at(t, 2 * p.j);
-    const uint32_t vw = *reinterpret_cast<const uint16_t*>(vp) | (uint32_t)*reinterpret_cast<const uint16_t*>(vp + 64) << 16;
+    const u32x2 kw = reinterpret_cast<const u32x2*>(a.cache.k + region * kPlane4 + key_at(t))[p.j];
+    const uint8_t* vp = a.cache.v + region * kPlane4 + value_at(t, 4 * p.j);
+    uint32_t vw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vw[i] = *reinterpret_cast<const uint16_t*>(vp + 64 * i);
     const uint8_t* sp = a.cache.scales + region * kScales4;
-    values8(kw, scale_of(sp[key_scale_at(t)]), k);
-    values8(vw, scale_of(sp[value_scale_at(t)]), v);
-    hadamard8<false>(k, p.j);
-    hadamard8<false>(v, p.j);
+    const float ks = scale_of(sp[key_scale_at(t)]), vs = scale_of(sp[value_scale_at(t)]);
+    values8(kw[0], ks, k);
+    values8(kw[1], ks, k + 8);
+    values8(vw[0] | vw[1] << 16, vs, v);
+    values8(vw[2] | vw[3] << 16, vs, v + 8);
+    hadamard16<false>(k, p.j);
+    hadamard16<false>(v, p.j);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) k[i] = v[i] = __builtin_nanf("");
+    for (int i = 0; i < 16; ++i) k[i] = v[i] = __builtin_nanf("");
   }
   const int64_t at = (((int64_t)p.l * a.rows + p.row) * a.heads + p.h) * kDim;
-  store_eight<OUT, false>(a.k_out, at, p.j, k);
-  store_eight<OUT, false>(a.v_out, at, p.j, v);
+  store_lane<OUT, false>(a.k_out, at, p.j, k);
+  store_lane<OUT, false>(a.v_out, at, p.j, v);
 }
 
 template <int IO>

@@ -2,7 +2,7 @@
 //
 // Of all probabilities two numbers per drafted token decide what is accepted, and one
 // row of the target and at most one of the draft what comes next. A sequence's row is
-// cut into chunks of 2048 entries and more, one per block. Every block finds the row by
+// cut into chunks of 2048 entries or a multiple, one per block. Every block finds the row by
 // itself (it needs a few numbers, and waiting for another block would cost more), sums
 // its chunk's weights, and the last block of a sequence to count itself in looks for the
 // chunk and then in it for the token. Small vocabularies take one block, one pass.
@@ -22,10 +22,6 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64, kEach = 8, kTile = kThreads * kEach;
 constexpr int kMaxChunks = 256;
 
-__host__ __device__ __forceinline__ int chunk_entries(int vocab) {
-  const int tiles = (vocab + kTile - 1) / kTile;
-  return (tiles + kMaxChunks - 1) / kMaxChunks * kTile;
-}
 
 // A probability as it counts.
 __device__ __forceinline__ float counted(float p) { return p > 0.0f && p < INFINITY ? p : 0.0f; }
@@ -42,7 +38,7 @@ __device__ __forceinline__ void load_probabilities(const void* base, int64_t row
   const int64_t at = row + first;
   const uint8_t* from = reinterpret_cast<const uint8_t*>(base) + at * io_bytes<IO>();
   if (first + kEach <= vocab && (reinterpret_cast<uintptr_t>(from) & 15) == 0) {
-    load_eight<IO, false>(base, at, 0, p);
+    load_run<IO>(base, at, p);
   } else {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) p[i] = first + i < vocab ? load_element<IO>(base, at + i) : 0.0f;
@@ -149,8 +145,39 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
     if (a.seq_len) a.keep[b] = a.seq_len[b] - drafts + accepted;
   }
 
+  const double share = (double)a.uniform_next[b];
+  // The token at which a thread's sums, on top of those before it, pass the border (the last one with a weight
+  // where none does).
+  auto store_token = [&](const double (&w)[kEach], double sum, double border, int first) {
+    int64_t token = -1;
+    bool over = false;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      sum += w[i];
+      if (w[i] > 0.0 && !over) {
+        token = first + t * kEach + i;
+        over = sum > border;
+      }
+    }
+    a.next[b] = token;
+  };
+  if (a.vocab <= kTile) {
+    double w[kEach], own, upto, total = 0.0;
+    for (int n = s.rejected ? 0 : 1; n < 2 && !(total > 0.0); ++n) {   // (all of the target counts where nothing is left of it)
+      weights<IO>(a, s, n == 0, t * kEach, w);
+      own = sum_of(w);
+      upto = scan(own, s_waves, total);
+    }
+    const int found = first_above(own > 0.0, upto > share * total, s_found);
+    if (t == max(found, 0)) {
+      if (found < 0) a.next[b] = -1;
+      else store_token(w, upto - own, share * total, 0);
+    }
+    return;
+  }
+
   // The chunk's sum, and the block that has them all.
-  const int entries = chunk_entries(a.vocab);
+  const int entries = a.entries;
   auto chunk_sum = [&](int c, bool difference) {
     double sum = 0.0;
     for (int first = c * entries; first < min((c + 1) * entries, a.vocab); first += kTile) {
@@ -181,9 +208,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
   __syncthreads();
 
   // The chunk that the border lies in. Where nothing is left of the target, all of it counts.
-  const double share = (double)a.uniform_next[b];
   bool difference = s.rejected;
-  int64_t token = -1;
   while (true) {
     const double own = t < a.chunks ? s_sums[t] : 0.0;
     double total;
@@ -217,19 +242,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
     weights<IO>(a, s, difference, first + t * kEach, w);
     const double own = sum_of(w), upto = scan(own, s_waves, total);
     const int found = first_above(own > 0.0, upto > rest, s_found);
-    if (t == found) {
-      double sum = upto - own;
-      bool over = false;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        sum += w[i];
-        if (w[i] > 0.0 && !over) {
-          token = first + t * kEach + i;       // (the last one with a weight where none is over)
-          over = sum > rest;
-        }
-      }
-      a.next[b] = token;
-    }
+    if (t == found) store_token(w, upto - own, rest, first);
     if (s_found[0] < kThreads) return;         // (what the block agrees on)
     rest -= total;
     __syncthreads();
@@ -238,9 +251,11 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
 
 }  // namespace
 
-int verify_chunks(int vocab) {
-  const int entries = chunk_entries(vocab);
-  return (vocab + entries - 1) / entries;
+int verify_entries(int vocab, int B) {
+  // Blocks for about twice the compute units, sixteen a sequence at least where the vocabulary has the tiles.
+  const int tiles = (vocab + kTile - 1) / kTile;
+  const int chunks = std::min(kMaxChunks, std::max(512 / B, 16));
+  return (tiles + chunks - 1) / chunks * kTile;
 }
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t st) {
