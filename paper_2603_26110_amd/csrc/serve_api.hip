@@ -91,8 +91,6 @@ bool too_many_stores(int32_t rows, int32_t nlayers, int32_t kv_heads) {
   return ((int64_t)rows + 63) / 64 > (((int64_t)1 << 24) - 1) / nlayers / kv_heads;
 }
 
-int chunks_of(int32_t vocab, int entries) { return (vocab + entries - 1) / entries; }
-
 tqp::Rows rows_of(const tqp_rows* r) { return tqp::Rows{r->data, r->layer_stride, r->row_stride, r->head_stride}; }
 
 tqp::Cache4Args cache_of(const tqs_cache* c) {
@@ -255,8 +253,7 @@ tq_status tqs_attend(const tqp_params* params, const tqs_cache* cache, const tqp
 
 size_t tqs_verify_workspace_bytes(int32_t vocab, int32_t B) {
   if (vocab < 1 || vocab > kMaxVocab || B < 1 || B > TQP_MAX_SEQS) return 0;
-  const int chunks = chunks_of(vocab, tqp::verify_entries(vocab, B));
-  return chunks == 1 ? 0 : tqp::kCounterBytes + (size_t)B * chunks * sizeof(double);
+  return tqp::plan_verify(vocab, B).workspace;
 }
 
 tq_status tqs_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int32_t io_dtype,
@@ -280,8 +277,8 @@ tq_status tqs_verify(const void* target, int64_t target_stride, const void* draf
   a.target = target; a.draft = draft;
   a.target_stride = target_stride; a.draft_stride = draft_stride;
   a.io = io_dtype; a.vocab = vocab; a.rows = rows; a.B = B;
-  a.entries = tqp::verify_entries(vocab, B);
-  a.chunks = chunks_of(vocab, a.entries);
+  const tqp::VerifyPlan plan = tqp::plan_verify(vocab, B);
+  a.entries = plan.entries; a.units = plan.units; a.chunks = plan.chunks;
   a.tokens = tokens; a.row0 = row0; a.uniform = uniform; a.uniform_next = uniform_next; a.seq_len = seq_len;
   a.accepted = accepted; a.next = next; a.keep = keep;
   if (need > 0) {

@@ -55,7 +55,7 @@ struct VerifyArgs {
   const void* draft;           // NULL: drafts are certain
   int64_t target_stride, draft_stride;
   int io, vocab, rows, B;
-  int entries, chunks;         // of a block; blocks of a sequence
+  int entries, units, chunks;  // entries of a unit, units of a block, blocks of a sequence
   const int64_t* tokens;
   const int32_t* row0;
   const float* uniform;
@@ -65,7 +65,7 @@ struct VerifyArgs {
   int64_t* next;
   int32_t* keep;
   uint32_t* counters;          // [B]
-  double* sums;                // [B][chunks]
+  double* sums;                // [B][units of a row]
 };
 
 hipError_t launch_norm_rope(const NormArgs& a, hipStream_t st);
@@ -73,7 +73,11 @@ hipError_t launch_append4(const StoreArgs& a, hipStream_t st);
 hipError_t launch_read4(const StoreArgs& a, hipStream_t st);
 AttendPlan plan_attend4(int64_t units0, int64_t rows_per_unit, int max_len);
 hipError_t launch_attend4(const Attend4Args& a, const AttendPlan& p, hipStream_t st);
-int verify_entries(int vocab, int B);        // entries of a block
+struct VerifyPlan {
+  int entries, units, chunks;
+  size_t workspace = 0;
+};
+VerifyPlan plan_verify(int vocab, int B);
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);
 
 }  // namespace tqp
