@@ -54,12 +54,6 @@ __device__ __forceinline__ f16x8 halves8(uint32_t lo, uint32_t hi, float by = 1.
 
 __device__ __forceinline__ f16x2 half2_of(_Float16 a, _Float16 b) { return f16x2{a, b}; }
 
-// What a sum of products is multiplied by: positive and finite, so that masked
-// scores stay -infinity and zeros stay zero.
-__device__ __forceinline__ float score_scale(float row, float page) {
-  return __builtin_amdgcn_fmed3f(row * page, 1e-37f, 3e38f);
-}
-
 // Sums O are in units of a page's value scale, and a page's values are at most
 // 448 * 2^47: with weights of W in all, |O| <= 2^56 W / scale. W is below 2^45
 // (2^30 tokens of 2^15), so that O stays within binary32 for scales from 2^-24

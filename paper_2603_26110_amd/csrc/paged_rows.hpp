@@ -243,6 +243,12 @@ __device__ __forceinline__ void split8(const float* x, int e, f16x8& hi, f16x8& 
   }
 }
 
+// What a sum of products is multiplied by: positive and finite, so that masked
+// scores stay -infinity and zeros stay zero.
+__device__ __forceinline__ float score_scale(float row, float page) {
+  return __builtin_amdgcn_fmed3f(row * page, 1e-37f, 3e38f);
+}
+
 // Bytes of the tokens first .. first+3 that are below len.
 __device__ __forceinline__ uint32_t below(int first, int len) {
   const int n = len - first;

@@ -32,13 +32,6 @@ constexpr float kRaise = 15.0f;
 
 __device__ __forceinline__ uint32_t bits_of(bf16x2 x) { return __builtin_bit_cast(uint32_t, x); }
 
-// Eight codes times a power of two (its exponent's bits) as bf16, exactly.
-__device__ __forceinline__ bf16x8 values_bf16(uint32_t w, float by) {
-  const u32x4 v = {bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 0)), bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 1)),
-                   bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 2)), bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 3))};
-  return __builtin_bit_cast(bf16x8, v);
-}
-
 // Two tokens' codes of four dimensions (16 bits each) as pairs of tokens: out[d] is
 // dimension d of both.
 __device__ __forceinline__ void values_pairs(uint32_t w, float by0, float by1, uint32_t (&out)[4]) {
@@ -66,10 +59,10 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&part)[PARTS]
   }
 }
 
-// Eight codes as fp16.
-__device__ __forceinline__ f16x8 codes_f16(uint32_t w) {
-  const u32x4 v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3))};
+// Eight codes as fp16, times a power of two.
+__device__ __forceinline__ f16x8 codes_f16(uint32_t w, float by = 1.0f) {
+  const u32x4 v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, by, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, by, 1)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, by, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, by, 3))};
   return __builtin_bit_cast(f16x8, v);
 }
 
@@ -107,22 +100,16 @@ __device__ __forceinline__ void hadamard_query(float (&x)[N]) {
   }
 }
 
-// Such entries as parts of eight an operand.
-template <int N, int PARTS>
-__device__ __forceinline__ void query_parts(const float (&x)[N], bf16x8 (&q)[PARTS][N / 8]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 8) {
-    u32x4 w[PARTS];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t p[PARTS];
-      split2<PARTS>(x[i + 2 * j], x[i + 2 * j + 1], p);
-#pragma unroll
-      for (int n = 0; n < PARTS; ++n) w[n][j] = p[n];
-    }
-#pragma unroll
-    for (int n = 0; n < PARTS; ++n) q[n][i / 8] = __builtin_bit_cast(bf16x8, w[n]);
-  }
+// The largest of 64 lanes' whole numbers, none negative, as a scalar.
+__device__ __forceinline__ int largest_of_wave(int x) {
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x128, 0xF, 0xF, true));   // (rotations of 16 by 8, 4, 2, 1)
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x124, 0xF, 0xF, true));
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x122, 0xF, 0xF, true));
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x121, 0xF, 0xF, true));
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max((int)a[0], (int)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return __builtin_amdgcn_readfirstlane(max((int)b[0], (int)b[1]));
 }
 
 // Weights exp2(s c - m). A multiply-add does not round s c, but m was rounded: from 2^25
@@ -456,9 +443,17 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
 
 // ------------------------------------------------------------ many rows
 // The waves of a group, 32 rows each, share a page: their threads load its codes,
-// convert them to bf16 and leave them in LDS as the matrix instructions take them (16
+// convert them and leave them in LDS as the matrix instructions take them (16
 // bytes a lane). While one page is worked on the next one's codes are on their way in
 // registers, and one barrier a page is enough for two buffers.
+//
+// Here scales go into the operands, once a page for all rows. Values are bf16, which has
+// binary32's exponents, so that a token's scale need not be brought in line with
+// another's; the weights are in one or more bf16 parts. Keys are fp16, so that a query in one part (2^-12
+// of an entry) is enough for bf16 results, over a power of two a page that puts its largest
+// scale at 2^13: exact for scales down to 2^-36 of it. A page with smaller ones has its codes
+// staged as they are and its scores multiplied afterwards (as whole numbers of the
+// largest are then a token's own).
 //
 // GROUPS: 1: one group of four waves, 128 rows a block. 2: two groups of two
 // waves, 64 rows a block, that take every other page each and are joined at the
@@ -466,13 +461,16 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
 // do not fill the chip.
 constexpr int kFrag = 64 * 16;                        // bytes of an operand of one instruction
 
+constexpr int kReach = 36, kHigh = 13;                // binades that a page's keys keep all bits in; of its largest scale
+
 template <int IO, int QPARTS, int WPARTS, int ROPE, int GROUPS>
-__global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid grid) {
+__global__ __launch_bounds__(256, GROUPS == 1 && WPARTS == 1 ? 4 : 2) void attend4_many(Attend4Args a, AttendGrid grid) {
   constexpr int kWaves = 4 / GROUPS, kThreads = 64 * kWaves;   // of a group
   constexpr int kBuffers = GROUPS == 2 && WPARTS < 3 ? 1 : 2;
   static_assert(2 * 34 * 64 * 4 <= 32 * kFrag && 2 * kRowsMany * kMaxSplit * 8 <= 32 * kFrag, "room for the groups' sums, and the splits'");
   // [group][buffer][keys: 32-token half T, step | values: 32-dimension half, step][lane]
   __shared__ __align__(16) uint8_t s_page[GROUPS * kBuffers * 16 * kFrag];
+  __shared__ float s_scale[GROUPS * kBuffers][kPage];  // of a page's keys, where they are applied to scores
   __shared__ int s_most[4];
   const Place place = place_of(a, grid);
   if (!place.there) return;
@@ -526,11 +524,11 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
   // (the token's place within an operand is turned by what the four threads of
   // a token differ in, so that their stores go to different banks)
   // Value operands: step u, lane (half, dimension): tokens 16 u + 4 half + r and
-  // 16 u + 8 + 4 half + r.
+  // 16 u + 8 + 4 half + r. (Their dimensions are turned within fours by what else differs between threads.)
   const int tg = threadIdx.x % kThreads;
   u32x2 kw[GROUPS], vw[GROUPS];
-  uint32_t ks[GROUPS], vs[GROUPS];             // a byte; four
-  uint32_t kto[GROUPS], vto[GROUPS], ksat[GROUPS], vsat[GROUPS];
+  uint32_t ks[GROUPS], vs[GROUPS], kall = 0;   // a byte; four; the byte of token 16 (lane % 4) + lane / 4
+  uint32_t kto[GROUPS], vto[GROUPS], vturn[GROUPS], ksat[GROUPS], vsat[GROUPS];
   int vtok[GROUPS];
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) {
@@ -539,6 +537,7 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
     ksat[i] = key_scale_at(tok);
     const int u = 2 * (at >> 7) + (at & 1), g = (at >> 1) & 3, vd = 4 * ((at >> 3) & 15);
     vto[i] = (8 + (vd >> 5) * 4 + u) * kFrag + ((g & 1) * 32 + (vd & 31)) * 16 + (g >> 1) * 8;
+    vturn[i] = ((u & 1) + 2 * (g & 1)) * 16;
     vtok[i] = 16 * u + 4 * g;
     vsat[i] = value_scale_at(vtok[i]);
   }
@@ -548,6 +547,7 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
     const u32x2* kp = reinterpret_cast<const u32x2*>(kplane + (int64_t)page * kPlane4) + tg;
     const u32x2* vp = reinterpret_cast<const u32x2*>(vplane + (int64_t)page * kPlane4) + tg;
     const uint8_t* sp = scales + (int64_t)page * kScales4;
+    kall = bad ? 255 : sp[lane];
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
       kw[i] = kp[i * kThreads];
@@ -560,18 +560,28 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
       }
     }
   };
-  auto stage = [&](uint8_t* to, int tl) {
+  // What scores of the page that is staged are multiplied by, and whether their tokens' scales are still to come.
+  float kscale = 1.0f;
+  bool wide = false;
+  auto stage = [&](int buffer, int tl) {
+    uint8_t* to = s_page + (group * kBuffers + buffer) * 16 * kFrag;
+    const bool counts = kall != 255 && tl * kPage + 16 * (lane & 3) + (lane >> 2) < s.len;
+    const int high = max(largest_of_wave(counts ? (int)kall : 0), 127 + kMinExp);
+    wide = __any(counts && high - (int)kall > kReach);
+    kscale = wide ? 1.0f : pow2(high - 127 - kHigh);
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
-      const float by = scale_of(ks[j]);
-      *reinterpret_cast<bf16x8*>(to + kto[j]) = values_bf16(kw[j][0], by);
-      *reinterpret_cast<bf16x8*>(to + kto[j] + kFrag) = values_bf16(kw[j][1], by);
+      // (NaN where the key is no number)
+      const float by = __uint_as_float(ks[j] == 255 ? kInfBits : wide ? 127u << 23 : (ks[j] + (127 + kHigh - high)) << 23);
+      *reinterpret_cast<f16x8*>(to + kto[j]) = codes_f16(kw[j][0], by);
+      *reinterpret_cast<f16x8*>(to + kto[j] + kFrag) = codes_f16(kw[j][1], by);
+      if (wide && (tg & 3) == 0) s_scale[group * kBuffers + buffer][(tg + j * kThreads) >> 2] = scale_of(ks[j]);
       if ((tl + 1) * kPage > s.len) vs[j] &= below(tl * kPage + vtok[j], s.len);
       uint32_t lo[4], hi[4];
       values_pairs(vw[j][0], scale_in(vs[j], 0), scale_in(vs[j], 1), lo);
       values_pairs(vw[j][1], scale_in(vs[j], 2), scale_in(vs[j], 3), hi);
 #pragma unroll
-      for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x2*>(to + vto[j] + d * 16) = u32x2{lo[d], hi[d]};
+      for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x2*>(to + vto[j] + ((d * 16) ^ vturn[j])) = u32x2{lo[d], hi[d]};
     }
   };
   int page = 0;                  // table entry of the page to load next
@@ -582,27 +592,35 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
   }
 
   // q': lane (half, column) has dimensions 32 half .. +31 of its row
-  bf16x8 q[QPARTS][4];
+  f16x8 qh[4], ql[4];
+  float rowscale;
   {
     float x[32];
     Query<IO, 32, ROPE> query;
     load_query(a, r, l, 32 * half, query);
     rotate_query(query, 32 * half, x);
     hadamard_query<32, 32>(x);
-    query_parts<32, QPARTS>(x, q);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = max(top, abs_bits(x[i]));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+    const int e = row_exponent<kBF16, kNone>(top);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split8<QPARTS - 1>(x + 8 * i, e, qh[i], ql[i]);
+    rowscale = a.scale2 * pow2(max(e, -126));
   }
 
   float m = lowest(), lsum = 0.0f;
   f32x16 O[2] = {};
+  const uint32_t vfrom[2] = {(uint32_t)(lane ^ (2 * half)) * 16, (uint32_t)(lane ^ (2 * half + 1)) * 16};
   const uint32_t kfrom[2] = {(uint32_t)(32 * half + (c32 ^ (8 * half))) * 16, (uint32_t)(32 * half + (c32 ^ (4 + 8 * half))) * 16};
-  auto frag = [&](const uint8_t* from, int i, uint32_t at) { return *reinterpret_cast<const bf16x8*>(from + i * kFrag + at); };
-
-  auto page_of = [&](int buffer) { return s_page + (group * kBuffers + buffer) * 16 * kFrag; };
-  if (begin < ntiles) stage(page_of(0), begin);
+  if (begin < ntiles) stage(0, begin);
   int buffer = 0;
   for (int tl = begin; tl < ntiles + group; tl += GROUPS, buffer = (buffer + 1) % kBuffers) {   // (the same turns for all groups)
-    const uint8_t* from = page_of(buffer);
-    const bool more = tl + GROUPS < ntiles;
+    const uint8_t* from = s_page + (group * kBuffers + buffer) * 16 * kFrag;
+    const float* after = s_scale[group * kBuffers + buffer];
+    const float pagescale = kscale;
+    const bool scaled = !wide, more = tl + GROUPS < ntiles;
     if (more) {
       load(page);
       page = table[min(tl + 2 * GROUPS, ntiles - 1)];
@@ -615,11 +633,17 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
         f32x16 z = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const bf16x8 kf = frag(from, 4 * T + i, kfrom[i >> 1]);
-#pragma unroll
-          for (int n = QPARTS - 1; n >= 0; --n) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n][i], z, 0, 0, 0);
+          const f16x8 kf = *reinterpret_cast<const f16x8*>(from + (4 * T + i) * kFrag + kfrom[i >> 1]);
+          if (QPARTS > 1) z = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[i], z, 0, 0, 0);
+          z = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qh[i], z, 0, 0, 0);
         }
         S[T] = z;
+      }
+      if (!scaled) {                // (uniform, and rare)
+#pragma unroll
+        for (int T = 0; T < 2; ++T)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) S[T][j] *= after[32 * T + 8 * (j >> 2) + 4 * half + (j & 3)];
       }
       if ((tl + 1) * kPage > least) {
 #pragma unroll
@@ -628,7 +652,7 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
           for (int j = 0; j < 16; ++j)
             if (tl * kPage + 32 * T + 8 * (j >> 2) + 4 * half + (j & 3) >= r.sees) S[T][j] = -INFINITY;
       }
-      float c = a.scale2, top = S[0][0];
+      float c = score_scale(rowscale, pagescale), top = S[0][0];
 #pragma unroll
       for (int T = 0; T < 2; ++T)
 #pragma unroll
@@ -664,7 +688,7 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
         }
 #pragma unroll
         for (int d = 0; d < 2; ++d) {
-          const bf16x8 vf = frag(from, 8 + 4 * d + u, lane * 16);
+          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(from + (8 + 4 * d + u) * kFrag + vfrom[u & 1]);
 #pragma unroll
           for (int p = WPARTS - 1; p >= 0; --p)
             O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pw[p]), O[d], 0, 0, 0);
@@ -672,7 +696,7 @@ __global__ __launch_bounds__(256, 2) void attend4_many(Attend4Args a, AttendGrid
       }
     }
     if (kBuffers == 1) __syncthreads();
-    if (more) stage(page_of((buffer + 1) % kBuffers), tl + GROUPS);
+    if (more) stage((buffer + 1) % kBuffers, tl + GROUPS);
   }
   lsum += __shfl_xor(lsum, 32, 64);
   if constexpr (GROUPS == 2) {
@@ -822,9 +846,10 @@ hipError_t launch(const Attend4Args& a, const AttendPlan& p, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_attend4(const Attend4Args& a, const AttendPlan& p, hipStream_t st) {
-  if (a.io == kF32) return launch<kF32, 3, 3>(a, p, st);
-  if (a.io == kF16) return a.out_f32 ? launch<kF16, 3, 3>(a, p, st) : launch<kF16, 2, 2>(a, p, st);
-  return a.out_f32 ? launch<kBF16, 3, 3>(a, p, st) : launch<kBF16, 2, 1>(a, p, st);
+  // (parts of a query in fp16, of a weight in bf16, for many rows)
+  if (a.io == kF32) return launch<kF32, 2, 3>(a, p, st);
+  if (a.io == kF16) return a.out_f32 ? launch<kF16, 2, 3>(a, p, st) : launch<kF16, 2, 2>(a, p, st);
+  return a.out_f32 ? launch<kBF16, 2, 3>(a, p, st) : launch<kBF16, 1, 1>(a, p, st);
 }
 
 }  // namespace tqp

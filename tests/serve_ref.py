@@ -148,18 +148,20 @@ def attend(k, v, q, pos, row0, table, seq_len, causal, scale, cs64=None, half=Fa
     return out @ had, spread.sum(-1, keepdim=True) / 8, size, reach
 
 
-def bound(out, spread, size, reach, length, parts, dtype):
-    """How far a result may be from the 64-bit one, elementwise. parts: bf16 parts of a query and of a weight.
+def bound(out, spread, size, reach, length, eps, dtype):
+    """How far a result may be from the 64-bit one, elementwise. eps: what the rounding of a query's entry and of a weight
+    leaves, relative to them.
 
-    A part rounds to 8 bits, so that n parts leave 2^-8n of a number. RoPE rounds three times for each entry and the
-    butterflies six, relative to the sum of the entries' sizes that go in: 10 * 2^-24 (entries' sizes grow by sqrt 2 in
-    a rotation) of reach in a score, and eps_q of its own size; the sum over 64 products and parts, the scaling and the
-    difference from the reference round at most 200 times 2^-24 of it. A weight has the score's error, the exp2's (2^-22)
-    and its own parts'; numerator and denominator both. Both sum `length` terms in fp32, a few parts each, and joins of
-    waves and splits scale them a few times. Errors of the numerator are relative to sum_j w_j |v_j| by dimension
-    of the Hadamard basis, and the way back sums them over the dimensions: `spread`; its own butterflies round seven
-    times more. Last the output's own rounding."""
-    eps = [2.0 ** (-8 * n) for n in parts]
+    RoPE rounds three times for each entry and the butterflies six, relative to the sum of the entries' sizes that go
+    in: 10 * 2^-24 (entries' sizes grow by sqrt 2 in a rotation) of reach in a score, and eps[0] of its own size (an entry's
+    rounding is relative to itself down to 2^-38 of its row's largest, the rest of which 2^-24 covers); the sum over 64 products
+    and parts, the scales and the difference from the reference round at most 200 times 2^-24 of it. A weight has the
+    score's error, the exp2's (2^-22) and its own rounding's; numerator and denominator both. Where weights are held in
+    fp16 its steps are 2^-32 of the largest w_j scale_j, each times a code of at most 6: for `length` tokens less than
+    the 2^-24 length of the sums, as spread is more than w_j scale_j for codes that are not nearly all zero. Both sum
+    `length` terms in fp32, a few parts each, and joins of waves and splits scale them a few times. Errors of the
+    numerator are relative to sum_j w_j |v_j| by dimension of the Hadamard basis, and the way back sums them over the
+    dimensions: `spread`; its own butterflies round seven times more. Last the output's own rounding."""
     score = eps[0] * size + 2.0 ** -24 * (200 * size + 15 * reach)
     rel = 2 * torch.expm1(score) + 2 * eps[1] + 2.0 ** -21 + (2 * 3 * length + 100) * 2.0 ** -24
     half = torch.finfo(dtype).eps / 2

@@ -11,7 +11,9 @@ from paper_2603_26110_amd import paged, serve
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
-PARTS = {F16: (2, 2), BF16: (2, 1), F32: (3, 3)}     # bf16 parts of a query and of a weight, at least
+# By the result's type: a query's entry in fp16, one part (2^-11) or two (2^-22); a weight in fp16 or bf16, one part (2^-11, 2^-8) or
+# more (fp32 results: 2^-22 at least)
+EPS = {F16: (2.0 ** -22, 2.0 ** -11), BF16: (2.0 ** -11, 2.0 ** -8), F32: (2.0 ** -22, 2.0 ** -22)}
 
 
 def i32(x):
@@ -183,9 +185,8 @@ def check_attend(L, H, G, lens, news, dtype, rope="none", causal=True, fp32_out=
     want, spread, size, reach = ref.attend(k, v, q.double(), pos, row0, table, lens, causal, scale,
                                            None if cs is None else angles(top), rope == "half")
     kind = F32 if fp32_out else dtype
-    parts = PARTS[kind]
     assert out.dtype == kind and out.shape == q.shape
-    off, most = (out.double() - want).abs(), ref.bound(want, spread, size, reach, max(lens), parts, kind)
+    off, most = (out.double() - want).abs(), ref.bound(want, spread, size, reach, max(lens), EPS[kind], kind)
     assert bool((off <= most).all()), (float((off - most).max()), float((off / most).max()))
     again = serve.attend(*args, causal=causal, layer0=layer0, workspace=room)
     assert torch.equal(out, again)                           # (the counters are zero again, and the order is fixed)
@@ -249,6 +250,26 @@ def test_attend_scales_of_all_sizes(new, dtype):
     check_attend(1, 2, 1, [200], [new], dtype, lo=124, hi=132, qsize=20.0, seed=7)     # scores in the thousands
 
 
+@pytest.mark.parametrize("new", [1, 100])
+@pytest.mark.parametrize("gap", [30, 36, 37, 60])
+def test_attend_small_keys_before_large_ones(new, gap):
+    # the page's last tokens have keys 2^gap times as large as the others: rows that do not see them keep all digits
+    n = 100
+    table, pos, row0, pages = layout([n], [new], 3)
+    cache = random_cache(1, 1, pages, 4, 120, 124)
+    for t in (62, 63, 90, 99):
+        cache.scales[0, 0, table[0][t // 64], int(ref.KEY_SCALE[t % 64])] = 122 + gap
+    params = paged.Params(1, 1, 1, io_dtype=F32)
+    q = rows_of((1, new, 1, 64), 7, F32, 2.0 ** -4)
+    out = serve.attend(params, cache, q, i32(pos), i32(row0), i32(table), i32([n]), new, n)
+    k, v = (torch.from_numpy(x).to(DEV) for x in ref.CacheRef(cache).values())
+    for p in range(n - new, n):
+        r = p - (n - new)
+        w, spread, size, reach = ref.attend(k, v, q[:, r:r + 1].double(), [p], [0, 1], table, [p + 1], True, 0.125)
+        off = (out[:, r:r + 1].double() - w).abs()
+        assert bool((off <= ref.bound(w, spread, size, reach, n, EPS[F32], F32)).all()), p
+
+
 @pytest.mark.parametrize("new,G", [(1, 3), (80, 1)])
 def test_attend_a_small_value_beside_a_large_one(new, G):
     # the large value's key is never looked at (a score of -2^14 or so against 2^14): the small values keep their digits
@@ -304,7 +325,7 @@ def test_attend_rows_that_are_not_valid(many):
     lens[3] = 0
     ref_q = q.double().nan_to_num(0, 0, 0)
     w, spread, size, reach = ref.attend(k, v, ref_q, [max(p, 0) % 300 for p in pos], row0, table, lens, True, 0.125, angles(300))
-    most = ref.bound(w, spread, size, reach, 200, PARTS[F16], F16)
+    most = ref.bound(w, spread, size, reach, 200, EPS[F16], F16)
     assert bool(((out.double() - w).abs() <= most)[0, good].all())
 
 
