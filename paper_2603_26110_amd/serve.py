@@ -30,12 +30,12 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
 from . import TQError
-from .paged import (_CAPACITY, _COUNTERS, _IO, MAX_SEQS, PAGE, Params, _check_rows, _dev, _fit, _Kept, _launch,
-                    _model_checks, _rows)
+from .paged import _CAPACITY, _COUNTERS, _IO, MAX_SEQS, PAGE, Params, _check_rows, _dev, _fit, _Kept, _launch, _model_checks
 
 __all__ = ["Cache4", "norm_rope", "append", "read", "attend", "verify", "workspace_bytes", "verify_workspace_bytes",
            "cache_bytes", "last_error", "lib_path", "MAX_AXES", "MAX_SEQS", "PAGE", "Params"]
@@ -121,6 +121,17 @@ def cache_bytes(num_layers: int, kv_heads: int, pages: int) -> int:
     return int(_load().tqs_cache_bytes(num_layers, kv_heads, pages))
 
 
+# As in the paged binding, the checks of a call's tensors are one expression, and only where that fails do they run one by
+# one, in order, to raise. Rows go to the library as the bytes of their structure (norm_rope hands over four of them).
+_pack_rows = struct.Struct("Pqqq").pack
+
+
+def _rows(t, shape) -> bytes:
+    s = t.stride()
+    # (the stride of a dimension of one entry says nothing)
+    return _pack_rows(t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+
+
 def norm_rope(params: Params, q, k, pos=None, q_weight=None, k_weight=None, eps: float = 1e-6, sections=None, out=None):
     """Norms every head of q [nlayers][rows][num_heads][64] and k [nlayers][rows][kv_heads][64] (divided by the root of
     the mean of its squares and eps, times ``q_weight`` or ``k_weight``, fp32 [nlayers][64] or None for ones) and
@@ -129,50 +140,63 @@ def norm_rope(params: Params, q, k, pos=None, q_weight=None, k_weight=None, eps:
     ``out``, two tensors of those shapes with strides in multiples of 8 elements: q and k themselves, say. What comes
     next takes params without a table."""
     L = _lib or _load()
-    io = params.io_dtype
-    if not isinstance(q, torch.Tensor) or not q.is_cuda:
-        raise TypeError("q must be a GPU tensor")
-    index = q.get_device()
-    _check_rows(q, "q", io, params.num_heads, index)
-    _check_rows(k, "k", io, params.kv_heads, index)
-    nlayers, rows = q.shape[:2]
-    if tuple(k.shape[:2]) != (nlayers, rows):
-        raise ValueError("q and k must have the same layers and rows")
-    if out is None:
-        out = torch.empty(q.shape, dtype=io, device=q.device), torch.empty(k.shape, dtype=io, device=q.device)
-    else:
-        for name, t, x in zip(("q out", "k out"), out, (q, k)):
-            _check_rows(t, name, io, x.shape[2], index)
-            if t.shape != x.shape:
-                raise ValueError(f"{name} must have the shape of its input")
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _dev(w, name, torch.float32, index)
-            if tuple(w.shape) != (nlayers, 64):
-                raise ValueError(f"{name} must be [{nlayers}][64]")
-    axes, parts = 1, None
-    if params.rope_cs is not None:
-        if params._index != index:
-            raise ValueError("rope_cs must be on the GPU of q")
-        _dev(pos, "pos", torch.int32, index)
-        if pos.dim() not in (1, 2) or pos.shape[-1] != rows:
+    io, heads, kv_heads = params.io_dtype, params.num_heads, params.kv_heads
+    turned = params.rope_cs is not None
+    try:
+        shape, kshape, index = q.shape, k.shape, q.get_device()
+        nlayers, rows = shape[0], shape[1]
+        fine = (q.dtype is io and k.dtype is io and index >= 0 and k.get_device() == index and len(shape) == 4
+                and len(kshape) == 4 and shape[2] == heads and kshape[2] == kv_heads and shape[3] == 64 and kshape[3] == 64
+                and kshape[0] == nlayers and kshape[1] == rows and q.stride(3) == 1 and k.stride(3) == 1
+                and (q_weight is None or (q_weight.dtype is torch.float32 and q_weight.shape == (nlayers, 64)
+                                          and q_weight.is_contiguous() and q_weight.get_device() == index))
+                and (k_weight is None or (k_weight.dtype is torch.float32 and k_weight.shape == (nlayers, 64)
+                                          and k_weight.is_contiguous() and k_weight.get_device() == index))
+                and (not turned or (params._index == index and pos.dtype is torch.int32 and pos.is_contiguous()
+                                    and pos.get_device() == index and 1 <= len(pos.shape) <= 2 and pos.shape[-1] == rows)))
+    except (AttributeError, IndexError):
+        fine = False
+    if not fine:
+        if not isinstance(q, torch.Tensor) or not q.is_cuda:
+            raise TypeError("q must be a GPU tensor")
+        index = q.get_device()
+        _check_rows(q, "q", io, heads, index)
+        _check_rows(k, "k", io, kv_heads, index)
+        if q.shape[:2] != k.shape[:2]:
+            raise ValueError("q and k must have the same layers and rows")
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None:
+                _dev(w, name, torch.float32, index)
+                if tuple(w.shape) != (q.shape[0], 64):
+                    raise ValueError(f"{name} must be [{q.shape[0]}][64]")
+        if turned:
+            if params._index != index:
+                raise ValueError("rope_cs must be on the GPU of q")
+            _dev(pos, "pos", torch.int32, index)
             raise ValueError("pos must be [rows] or [axes][rows]")
-        axes = pos.shape[0] if pos.dim() == 2 else 1
+    axes, parts = 1, None
+    if turned:
+        axes = pos.shape[0] if len(pos.shape) == 2 else 1
         if sections is not None:
             sections = [int(n) for n in sections]
             if len(sections) != axes:
                 raise ValueError("sections must have an entry for each axis of pos")
-            _fit(*sections)
-            parts = (ctypes.c_int32 * axes)(*sections)
-        elif axes > 1:
+            _fit(0, *sections)
+            parts = struct.pack(f"{axes}i", *sections)
+        elif axes != 1:
             raise ValueError("several axes need sections")
+    if out is None:
+        q_out, k_out = torch.empty(shape, dtype=io, device=q.device), torch.empty(kshape, dtype=io, device=q.device)
+    else:
+        q_out, k_out = out
+        for name, t, x in (("q out", q_out, q), ("k out", k_out, k)):
+            _check_rows(t, name, io, x.shape[2], index)
+            if t.shape != x.shape:
+                raise ValueError(f"{name} must have the shape of its input")
     _fit(rows, nlayers)
-    q_out, k_out = out
-    _check(_launch(index, L.tqs_norm_rope, ctypes.byref(params._c), ctypes.byref(_rows(q, q.shape)),
-                   ctypes.byref(_rows(k, k.shape)), rows, nlayers, None if q_weight is None else q_weight.data_ptr(),
-                   None if k_weight is None else k_weight.data_ptr(), eps,
-                   None if params.rope_cs is None else pos.data_ptr(), axes, parts,
-                   ctypes.byref(_rows(q_out, q.shape)), ctypes.byref(_rows(k_out, k.shape))))
+    _check(_launch(index, L.tqs_norm_rope, ctypes.byref(params._c), _rows(q, shape), _rows(k, kshape), rows, nlayers,
+                   None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+                   eps, pos.data_ptr() if turned else None, axes, parts, _rows(q_out, shape), _rows(k_out, kshape)))
     return q_out, k_out
 
 
@@ -182,19 +206,28 @@ def append(params: Params, cache: Cache4, k, v, slots, pos=None, layer0: int = 0
     multiples of 8 elements)."""
     L = _lib or _load()
     index = _model_checks(params, cache, Cache4)
-    io, heads = params.io_dtype, params.kv_heads
-    _check_rows(k, "k", io, heads, index)
-    _check_rows(v, "v", io, heads, index)
-    shape = k.shape
-    if shape != v.shape:
-        raise ValueError("k and v must have the same shape")
-    _dev(slots, "slots", torch.int64, index, shape[1])
-    if params.rope_cs is not None:
-        _dev(pos, "pos", torch.int32, index, shape[1])
-    _fit(shape[1], layer0, shape[0])
-    _check(_launch(index, L.tqs_append, ctypes.byref(params._c), ctypes.byref(cache._c), ctypes.byref(_rows(k, shape)),
-                   ctypes.byref(_rows(v, shape)), shape[1], layer0, shape[0], slots.data_ptr(),
-                   None if params.rope_cs is None else pos.data_ptr()))
+    io, heads, turned = params.io_dtype, params.kv_heads, params.rope_cs is not None
+    try:
+        shape = k.shape
+        rows = shape[1]
+        fine = (k.dtype is io and v.dtype is io and slots.dtype is torch.int64 and len(shape) == 4 and shape[3] == 64
+                and shape[2] == heads and v.shape == shape and k.stride(3) == 1 and v.stride(3) == 1
+                and slots.is_contiguous() and index >= 0 and k.get_device() == index and v.get_device() == index
+                and slots.get_device() == index and slots.numel() >= rows
+                and (not turned or (pos.dtype is torch.int32 and pos.is_contiguous() and pos.get_device() == index
+                                    and pos.numel() >= rows)))
+    except (AttributeError, IndexError):
+        fine = False
+    if not fine:
+        _check_rows(k, "k", io, heads, index)
+        _check_rows(v, "v", io, heads, index)
+        if k.shape != v.shape:
+            raise ValueError("k and v must have the same shape")
+        _dev(slots, "slots", torch.int64, index, rows)
+        _dev(pos, "pos", torch.int32, index, rows)
+    _fit(rows, layer0, shape[0])
+    _check(_launch(index, L.tqs_append, ctypes.byref(params._c), ctypes.byref(cache._c), _rows(k, shape), _rows(v, shape),
+                   rows, layer0, shape[0], slots.data_ptr(), pos.data_ptr() if turned else None))
 
 
 def read(params: Params, cache: Cache4, slots, layer0: int = 0, nlayers: int | None = None, out=None):
@@ -261,15 +294,26 @@ def attend(params: Params, cache: Cache4, q, pos, row0, table, seq_len, max_new:
     out [nlayers][rows][num_heads][64]."""
     L = _lib or _load()
     index = _model_checks(params, cache, Cache4)
-    _check_rows(q, "q", params.io_dtype, params.num_heads, index)
-    _dev(table, "table", torch.int32, index)
-    if table.dim() != 2:
-        raise ValueError("table must be [B][width]")
-    shape = q.shape
-    rows, (B, width) = shape[1], table.shape
-    _dev(pos, "pos", torch.int32, index, rows)
-    _dev(row0, "row0", torch.int32, index, B + 1)
-    _dev(seq_len, "seq_len", torch.int32, index, B)
+    io, heads, i32 = params.io_dtype, params.num_heads, torch.int32
+    try:
+        shape = q.shape
+        rows, (B, width) = shape[1], table.shape
+        fine = (q.dtype is io and len(shape) == 4 and shape[3] == 64 and shape[2] == heads and q.stride(3) == 1
+                and pos.dtype is i32 and row0.dtype is i32 and table.dtype is i32 and seq_len.dtype is i32
+                and pos.is_contiguous() and row0.is_contiguous() and table.is_contiguous()
+                and seq_len.is_contiguous() and index >= 0 and q.get_device() == index and pos.get_device() == index
+                and row0.get_device() == index and table.get_device() == index and seq_len.get_device() == index
+                and pos.numel() >= rows and row0.numel() > B and seq_len.numel() >= B)
+    except (AttributeError, IndexError, ValueError):
+        fine = False
+    if not fine:
+        _check_rows(q, "q", io, heads, index)
+        _dev(table, "table", i32, index)
+        if table.dim() != 2:
+            raise ValueError("table must be [B][width]")
+        _dev(pos, "pos", i32, index, q.shape[1])
+        _dev(row0, "row0", i32, index, table.shape[0] + 1)
+        _dev(seq_len, "seq_len", i32, index, table.shape[0])
     max_new, max_len = int(max_new), int(max_len)
     _fit(rows, B, width, layer0, shape[0], max_new, max_len)
     if out is None:
@@ -279,7 +323,7 @@ def attend(params: Params, cache: Cache4, q, pos, row0, table, seq_len, max_new:
         if out.shape != shape:
             raise ValueError("out must have the shape of q")
     at, size = _workspace(workspace, index)
-    args = (ctypes.byref(params._c), ctypes.byref(cache._c), ctypes.byref(_rows(q, shape)), rows, B, layer0, shape[0],
+    args = (ctypes.byref(params._c), ctypes.byref(cache._c), _rows(q, shape), rows, B, layer0, shape[0],
             pos.data_ptr(), row0.data_ptr(), table.data_ptr(), width, seq_len.data_ptr(), max_new, max_len,
             1 if causal else 0, out.data_ptr())
     status = _launch(index, L.tqs_attend, *args, at, size)
@@ -292,8 +336,8 @@ def attend(params: Params, cache: Cache4, q, pos, row0, table, seq_len, max_new:
     return out
 
 
-def _probabilities(t, name: str, dtype, shape, index: int) -> int:
-    """The row stride of a [rows][vocab] tensor."""
+def _check_probabilities(t, name: str, dtype, shape, index: int) -> None:
+    """Raises unless t is a [rows][vocab] tensor of strides that the library takes."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if t.dtype is not dtype:
@@ -304,7 +348,6 @@ def _probabilities(t, name: str, dtype, shape, index: int) -> int:
         raise ValueError(f"{name} must be on GPU {index}, got {t.device}")
     if shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the probabilities of a row must be contiguous")
-    return t.stride(0) if shape[0] > 1 else shape[1]
 
 
 def verify(target, draft, tokens, row0, uniform, uniform_next, seq_len=None, workspace=None):
@@ -316,29 +359,46 @@ def verify(target, draft, tokens, row0, uniform, uniform_next, seq_len=None, wor
     ``seq_len`` int32 [B] counts the rows in, and None without it. ``workspace``: as attend()'s, of
     verify_workspace_bytes(...) bytes."""
     L = _lib or _load()
-    if not isinstance(target, torch.Tensor) or not target.is_cuda:
-        raise TypeError("target must be a GPU tensor")
-    index, dtype = target.get_device(), target.dtype
-    if dtype not in _IO:
-        raise TypeError(f"target must be one of {[str(d) for d in _IO]}")
-    if target.dim() != 2:
-        raise ValueError("target must be [rows][vocab]")
-    shape = target.shape
-    strides = [_probabilities(target, "target", dtype, shape, index),
-               shape[1] if draft is None else _probabilities(draft, "draft", dtype, shape, index)]
-    rows, vocab = shape
-    _dev(row0, "row0", torch.int32, index, 1)
-    B = row0.numel() - 1
-    _dev(tokens, "tokens", torch.int64, index, rows)
-    _dev(uniform, "uniform", torch.float32, index, rows)
-    _dev(uniform_next, "uniform_next", torch.float32, index, B)
-    if seq_len is not None:
-        _dev(seq_len, "seq_len", torch.int32, index, B)
+    i32, f32 = torch.int32, torch.float32
+    try:
+        index, dtype, shape = target.get_device(), target.dtype, target.shape
+        rows, vocab = shape
+        B = row0.numel() - 1
+        fine = (index >= 0 and dtype in _IO and (vocab == 1 or target.stride(1) == 1)
+                and (draft is None or (draft.dtype is dtype and draft.shape == shape and draft.get_device() == index
+                                       and (vocab == 1 or draft.stride(1) == 1)))
+                and tokens.dtype is torch.int64 and row0.dtype is i32 and uniform.dtype is f32 and uniform_next.dtype is f32
+                and tokens.is_contiguous() and row0.is_contiguous() and uniform.is_contiguous()
+                and uniform_next.is_contiguous() and tokens.get_device() == index and row0.get_device() == index
+                and uniform.get_device() == index and uniform_next.get_device() == index and tokens.numel() >= rows
+                and B >= 0 and uniform.numel() >= rows and uniform_next.numel() >= B
+                and (seq_len is None or (seq_len.dtype is i32 and seq_len.is_contiguous()
+                                         and seq_len.get_device() == index and seq_len.numel() >= B)))
+    except (AttributeError, ValueError):
+        fine = False
+    if not fine:
+        if not isinstance(target, torch.Tensor) or not target.is_cuda:
+            raise TypeError("target must be a GPU tensor")
+        if target.dtype not in _IO:
+            raise TypeError(f"target must be one of {[str(d) for d in _IO]}")
+        if target.dim() != 2:
+            raise ValueError("target must be [rows][vocab]")
+        _check_probabilities(target, "target", target.dtype, target.shape, target.get_device())
+        if draft is not None:
+            _check_probabilities(draft, "draft", target.dtype, target.shape, target.get_device())
+        index, rows = target.get_device(), target.shape[0]
+        _dev(row0, "row0", i32, index, 1)
+        _dev(tokens, "tokens", torch.int64, index, rows)
+        _dev(uniform, "uniform", f32, index, rows)
+        _dev(uniform_next, "uniform_next", f32, index, row0.numel() - 1)
+        _dev(seq_len, "seq_len", i32, index, row0.numel() - 1)
     _fit(rows, vocab, B)
     at, size = _workspace(workspace, index)
     device = target.device
-    accepted, keep = torch.empty((2, B), dtype=torch.int32, device=device).unbind(0)
+    out = torch.empty((2, B), dtype=i32, device=device)
+    accepted, keep = out[0], out[1]
     token = torch.empty(B, dtype=torch.int64, device=device)
+    strides = [t.stride(0) if t is not None and rows > 1 else vocab for t in (target, draft)]
     args = (target.data_ptr(), strides[0], None if draft is None else draft.data_ptr(), strides[1], _IO[dtype], vocab,
             rows, B, tokens.data_ptr(), row0.data_ptr(), uniform.data_ptr(), uniform_next.data_ptr(),
             None if seq_len is None else seq_len.data_ptr(), accepted.data_ptr(), token.data_ptr(),
