@@ -8,10 +8,15 @@
 // rows a unit (one query token per sequence and its group of heads) a page per wave and
 // tiles of 16 rows, for many rows pages shared in LDS and 32 rows a wave.
 //
-// A code times its token's scale has two significant bits and binary32's exponents:
-// bf16 holds it exactly, so that no token's scale has to be brought in line with
-// another's, and no sum is in units of a page. Queries and weights enter as sums of
-// bf16 parts: one leaves 2^-8 of a number at most, two 2^-16, three 2^-24.
+// A code has two significant bits, and scales are powers of two, so that nothing of the
+// cache is rounded; what is, is in one or more parts: fp16 leaves 2^-11 of a number at most, two
+// parts 2^-22; bf16 2^-8, two parts 2^-16, three 2^-24.
+//
+// Measured: 640 (sequence, head) of 8192 tokens (346 MB) 60 us, 5.8 TB/s, where a plain read
+// of as much takes 57 (the 8-bit cache 119); 660 of 1025 tokens 14 us (19); 20 of 1025 tokens
+// 8.3 us, a chain of latencies; 512 ragged ones of up to 2001 tokens and five rows 19 us. Four
+// chunks of up to 512 rows on up to 4000 tokens (33 GFLOP), bf16 83 us; every token of 1024
+// with every other in 33 layers of 20 heads (177 GFLOP), bf16 339 us, fp16 490.
 //
 // The cache is in the Hadamard basis. A query row is brought there once (64 entries,
 // six butterflies, mostly within a lane), its result back once.

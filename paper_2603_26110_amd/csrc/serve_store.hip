@@ -8,7 +8,13 @@
 // groups of a wave have sixteen rows of one head: a value plane keeps the bytes of four
 // tokens side by side.
 //
-// The least traffic is 256 bytes of fp16 in and 66 out per token and head.
+// The least traffic is 256 bytes of fp16 in and 66 out per token and head. Measured: 33
+// 600 rows of 8 heads, bf16 (87 MB either way) in 27 us, out 20.5, where a copy of as much
+// takes 17; one row of 16 sequences 3.6 and 3.1 us. The append is bound in part by its
+// vector work (about 500 instructions for 16 token-heads) and by the value stores, two bytes
+// at a time: what a quarter of a wave's lanes store lies side by side for four tokens, which
+// saves the attention a transposition. (Eight lanes a vector 28.8 and 23.4 us; loads past the
+// caches 32 in, stores past them 31 out.)
 #include <algorithm>
 
 #include "serve_device.hpp"

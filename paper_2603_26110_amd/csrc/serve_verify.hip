@@ -12,7 +12,11 @@
 // 10^-7 of the total, and binary32 would move it. The order of the sums is fixed, whichever
 // block is last.
 // Bound by its chain of dependent loads and steps: row offsets, tokens, their
-// probabilities, the row, sums and counter, the unit, the token.
+// probabilities, the row, sums and counter, the unit, the token. Measured: 32 sequences
+// of up to six drafts over 131 072 tokens, fp32 (26 MB) 16.0 us, where a read of as much takes
+// 5; 8 over 33 symbols 5.4 us. (One tile a block 28 us, four a block with the token looked
+// for in all four 22.5; two, four and eight units a block 20.4, 16.0 and 18.1. Counters in lines of their
+// own changed nothing.)
 #include <algorithm>
 
 #include "serve_device.hpp"
