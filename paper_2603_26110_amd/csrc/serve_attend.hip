@@ -777,9 +777,11 @@ __global__ __launch_bounds__(256, GROUPS == 1 && WPARTS == 1 ? 4 : 2) void atten
 AttendPlan plan_attend4(int64_t units0, int64_t rows, int max_len) {
   AttendPlan p{};
   p.few = rows <= 64;
-  // Blocks of 128 rows where these fill the chip three times, else of 64.
+  // Blocks of 128 rows where these fill the chip three times, else of 64 (640 blocks of four
+  // chunks 100 us against 88). Tiles of one row and of four where a unit has no more (33 layers of
+  // 1025 tokens 14.5 us; 17.9 in a tile of four, 18.6 in one of sixteen).
   p.groups = units0 * ((rows + 4 * kRowsMany - 1) / (4 * kRowsMany)) < 768 ? 2 : 1;
-  const int per = !p.few ? 4 * kRowsMany / p.groups : rows <= 4 ? (int)(rows == 1 ? 1 : 4) : 16;
+  const int per = !p.few ? 4 * kRowsMany / p.groups : rows > 4 ? 16 : rows > 1 ? 4 : 1;
   p.rows = per;
   p.tiles = (int)((rows + per - 1) / per);
   p.units = units0 * p.tiles;
@@ -787,11 +789,16 @@ AttendPlan plan_attend4(int64_t units0, int64_t rows, int max_len) {
   p.waves = 4;
   const int64_t pages = std::max<int64_t>((max_len + (int64_t)kPage - 1) / kPage, 1);
   if (!p.few) {
+    // Long sequences of few rows are shared by blocks (13 heads, 100 rows on 8000 tokens 121 -> 41 us).
     const int64_t split = std::min<int64_t>(std::min<int64_t>(640 / p.units, pages / 16), kMaxSplit);
     if (p.groups == 2 && split > 1 && pages * (split - 1) >= 20 * split) p.nsplit = (int)split;
     if (p.nsplit > 1) p.workspace = kCounterBytes + (size_t)p.units * p.nsplit * (2 * kRowsMany) * kPartRow * sizeof(float);
     return p;
   }
+  // Eight waves a block where the units leave compute units free and there are pages for them
+  // (160 units of 128 pages 35.2 -> 23.8 us, 128 of 32 14.8 -> 14.3; 640 of 128 would go 67 -> 75); one
+  // where many units have few pages for it (10 560 of two pages 64 -> 27, 2400 of eight 24.4 ->
+  // 19.2).
   if (p.units <= 256 && pages >= 16) p.waves = 8;
   if (pages <= 8 && p.units >= 2048) p.waves = 1;
   // A unit's pages are shared by blocks where these find free compute units and each wave is
@@ -825,7 +832,8 @@ hipError_t launch(const Attend4Args& a, const AttendPlan& p, hipStream_t st) {
   g.units = (int)(p.units / p.tiles);
   g.tiles = p.tiles;
   g.by_xcd = g.units % kXcds == 0 || g.units >= 8 * kXcds;
-  // (where blocks differ, by what their rows see or by their sequences' lengths, and there are units enough)
+  // Where blocks differ, by what their rows see or by their sequences' lengths, and there are units
+  // enough (64 ragged prompts of 20 heads 259 -> 203 us).
   g.spread = !p.few && (a.causal || a.B > 1) && g.units >= 64 * kXcds;
   const int64_t lines = g.by_xcd ? (g.units + kXcds - 1) / kXcds * kXcds : g.units;
   const dim3 grid((unsigned)(lines * p.tiles * p.nsplit)), block(p.waves * 64);

@@ -18,7 +18,7 @@ residual magnitudes of the per-element sign correction come from
 tq_calibrate_ebar on the same calibration vectors. Calibration vectors are drawn from the same
 distributions at seeded positions.
 
-The command's last row is the paged 8-bit cache on the same inputs.
+The command's last rows are the paged 8-bit cache and the paged 4-bit one on the same inputs.
 
     python -m paper_2603_26110_amd.quality [--heads 20] [--tokens 1024] [--calib 4096]
 """
@@ -141,24 +141,25 @@ def decode_variant(inp: dict, var: dict) -> np.ndarray:
     return out.double().cpu().numpy()[0, 0]
 
 
-def decode_paged(inp: dict) -> np.ndarray:
-    """The paged 8-bit cache in the place of the 3-bit one (no rotation, tables or
-    signs): pages and slots for the T tokens by paged.assign, paged.append, then
-    paged.attend of the query at position T - 1 (fp32 output): [H][64]."""
+def decode_paged(inp: dict, bits: int = 8) -> np.ndarray:
+    """A paged cache of 8 or 4 bits in the place of the 3-bit one (no calibrated
+    rotation, tables or signs): pages and slots for the T tokens by paged.assign,
+    append, then attend of the query at position T - 1 (fp32 output): [H][64]."""
     import paper_2603_26110_amd as tq
-    from . import paged
+    from . import paged, serve
     dev = torch.device("cuda")
     H, T = inp["H"], inp["T"]
     t_ = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(dev)
     i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=dev)
     pages = (T + paged.PAGE - 1) // paged.PAGE
     params = paged.Params(1, H, H, tq.rope_table(T), io_dtype=torch.float16, flags=paged.OUT_FP32)
-    pool, cache = paged.PagePool(pages), paged.Cache(1, H, pages)
+    calls = paged if bits == 8 else serve
+    pool, cache = paged.PagePool(pages), (paged.Cache if bits == 8 else serve.Cache4)(1, H, pages)
     table, seq_len = torch.full((1, pages), -1, dtype=torch.int32, device=dev), i32(0)
     slots, pos, _, granted = paged.assign(pool, table, seq_len, i32(T), T)
     assert granted.item() == 1
-    paged.append(params, cache, t_(inp["k"][0]), t_(inp["v"][0]), slots, pos)
-    out = paged.attend(params, cache, t_(inp["q"]), i32(T - 1), i32(0, 1), table, seq_len, 1, T)
+    calls.append(params, cache, t_(inp["k"][0]), t_(inp["v"][0]), slots, pos)
+    out = calls.attend(params, cache, t_(inp["q"]), i32(T - 1), i32(0, 1), table, seq_len, 1, T)
     return out.double().cpu().numpy()[0, 0]
 
 
@@ -250,9 +251,10 @@ def main():
     for r in rows:
         print(f"| {r['variant']} | {r['cos_mean']:.5f} | {r['cos_min']:.5f} | {r['rel_l2']:.4f} |")
     inp = inputs(a.heads, a.tokens, a.calib, a.seed)
-    r = metrics(decode_paged(inp), inp["ref"])
-    print(f"| paged 8-bit cache (e4m3, a scale per page and head) | {r['cos_mean']:.5f} | {r['cos_min']:.5f} | "
-          f"{r['rel_l2']:.4f} |")
+    for bits, name in ((8, "paged 8-bit cache (e4m3, a scale per page and head)"),
+                       (4, "paged 4-bit cache (e2m1, Hadamard basis, a scale per token and head)")):
+        r = metrics(decode_paged(inp, bits), inp["ref"])
+        print(f"| {name} | {r['cos_mean']:.5f} | {r['cos_min']:.5f} | {r['rel_l2']:.4f} |")
 
 
 if __name__ == "__main__":

@@ -601,6 +601,22 @@ def test_a_serving_loop_with_drafts():
     assert pool.state.tolist() == [40 - used, 0, 0, 0]
 
 
+def test_the_quality_command_s_row_is_the_cache_s():
+    # the output of quality.decode_paged is the exact attention over what the cache holds, and above every 3-bit variant's
+    # worst case; the bound is that of the attention tests
+    from paper_2603_26110_amd import quality
+    inp = quality.inputs(heads=4, tokens=256, calib=64, seed=7)
+    got = quality.decode_paged(inp, 4)
+    cache, params = serve.Cache4(1, 4, 4), paged.Params(1, 4, 4, tq.rope_table(256))
+    k, v, q = (torch.from_numpy(np.ascontiguousarray(inp[n][0])).to(DEV) for n in ("k", "v", "q"))
+    serve.append(params, cache, k, v, i64(list(range(256))), i32(list(range(256))))
+    kr, vr = (torch.from_numpy(x).to(DEV) for x in ref.CacheRef(cache).values())
+    w, spread, size, reach = ref.attend(kr, vr, q[None].double(), [255], [0, 1], [[0, 1, 2, 3]], [256], True, 0.125, angles(256))
+    most = ref.bound(w, spread, size, reach, 256, EPS[F32], F32)[0, 0].cpu().numpy()
+    assert (np.abs(got - w[0, 0].cpu().numpy()) <= most).all()
+    assert quality.metrics(got, inp["ref"])["rel_l2"] > quality.metrics(quality.decode_paged(inp), inp["ref"])["rel_l2"]
+
+
 def test_a_captured_step():
     # norm, append, attend and verify in one graph, replayed with new inputs and eager work between
     L, H, Hkv, B, vocab = 1, 8, 2, 3, 5000
