@@ -64,7 +64,8 @@ TQ_API int64_t tqs_cache_bytes(int32_t num_layers, int32_t kv_heads, int64_t pag
 /* Norms every head of q and k and rotates it by its row's positions:
  *   y = x * weight / sqrt(mean(x^2) + eps)     (mean over the 64 dimensions)
  *   pair m of y is turned by the angle of params->rope_cs[pos[axis(m)][row]][m]
- * in binary32, rounded once to io_dtype. Pairs are (2m, 2m+1), or (m, m+32)
+ * in binary32, rounded once to io_dtype. (The squares are, too: entries past 2^60
+ * may overflow them, and with eps 0 a head of zeros is NaN.) Pairs are (2m, 2m+1), or (m, m+32)
  * with TQ_ROPE_HALF. The first sections[0] pairs take axis 0, the next
  * sections[1] axis 1, and so on (time, height and width, say). Without rope_cs
  * nothing is turned. What comes out goes to tqs_append, tqs_attend and their
@@ -74,7 +75,8 @@ TQ_API int64_t tqs_cache_bytes(int32_t num_layers, int32_t kv_heads, int64_t pag
  *
  *   q      device rows [nlayers][rows][num_heads][64] of io_dtype, k the same
  *          with kv_heads. q_out, k_out: where the results go, rows likewise;
- *          they may be q and k themselves, but not overlap them otherwise.
+ *          they may be q and k themselves, but not overlap them otherwise. (A
+ *          stride of zero over more than one row, head or layer is refused.)
  *   q_weight, k_weight  device fp32 [nlayers][64], 16-byte aligned, or NULL
  *          for ones.   eps >= 0, finite.
  *   pos    device int32 [axes][rows]; NULL only without rope_cs.
@@ -129,10 +131,12 @@ TQ_API tq_status tqs_read(const tqp_params* params, const tqs_cache* cache, cons
  * v_j of token j of the sequence (page table[b][j / 64]):
  *   s_j = softmax_scale * q'.k_j,  j < seq_len[b], and j <= pos[t] if causal
  *   out = sum_j softmax(s)_j v_j;  0 where there is no such j.
- * Sums and softmax statistics are in binary32. Codes times scales are bf16
- * values and enter the matrix cores as such; H q' / 8 enters them in two bf16
- * parts (2^-16), the weights in one (bf16 results of more than 64 rows a unit,
- * see max_new) or two; for fp32 results both in three.
+ * Sums and softmax statistics are in binary32, and the cache's values are used
+ * exactly. Up to 64 rows of max_new * num_heads / kv_heads, H q' / 8 enters the
+ * matrix cores as fp16 in two parts (2^-22) and a weight, times its value's scale,
+ * in one (2^-11; fp32 results: two). For more rows H q' / 8 is in one part for bf16
+ * results, else in two, and weights are bf16 in one part (2^-8) for bf16 results, two
+ * (2^-16) for fp16 and three for fp32.
  *   NaN: the rows of a sequence whose length is negative, above max_len or
  *   above 64*table_width or which has more than max_new rows; a row with
  *   pos < 0, or (with rope_cs) pos >= rope_positions; a row that sees a token

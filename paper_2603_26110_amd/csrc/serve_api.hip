@@ -81,6 +81,15 @@ tq_status check_rows(const tqp_rows* r, const char* name) {
   return TQ_OK;
 }
 
+// Rows to write to: heads of their own memory.
+tq_status check_out(const tqp_rows* r, const char* name, int32_t nlayers, int32_t rows, int32_t heads) {
+  const tq_status s = check_rows(r, name);
+  if (s != TQ_OK) return s;
+  if ((nlayers > 1 && r->layer_stride == 0) || (rows > 1 && r->row_stride == 0) || (heads > 1 && r->head_stride == 0))
+    return fail(TQ_ERR_ARG, "%s: a stride of zero", name);
+  return TQ_OK;
+}
+
 // (layer, sequence, key/value head)s and the rows of each are counted in 32 bits.
 bool too_many_units(int32_t nlayers, int32_t B, int32_t kv_heads, int64_t unit_rows) {
   return B > (((int64_t)1 << 30) - 1) / nlayers / kv_heads || unit_rows >= ((int64_t)1 << 30);
@@ -140,11 +149,12 @@ tq_status tqs_norm_rope(const tqp_params* params, const tqp_rows* q, const tqp_r
   }
   if (rows == 0 || nlayers == 0) return ok();
   if ((s = check_rows(q, "q")) != TQ_OK || (s = check_rows(k, "k")) != TQ_OK) return s;
-  if ((s = check_rows(q_out, "q_out")) != TQ_OK || (s = check_rows(k_out, "k_out")) != TQ_OK) return s;
-  if (params->rope_cs && !pos) return fail(TQ_ERR_ARG, "pos is NULL");
-  if (!aligned(q_weight, 16) || !aligned(k_weight, 16)) return fail(TQ_ERR_ALIGN, "weights must be 16-byte aligned");
   const int64_t eights = ((int64_t)params->num_heads + params->kv_heads + 7) / 8;
   if (rows > (((int64_t)1 << 26) - 1) / nlayers / eights) return fail(TQ_ERR_ARG, "too many rows for one call");
+  if ((s = check_out(q_out, "q_out", nlayers, rows, params->num_heads)) != TQ_OK) return s;
+  if ((s = check_out(k_out, "k_out", nlayers, rows, params->kv_heads)) != TQ_OK) return s;
+  if (params->rope_cs && !pos) return fail(TQ_ERR_ARG, "pos is NULL");
+  if (!aligned(q_weight, 16) || !aligned(k_weight, 16)) return fail(TQ_ERR_ALIGN, "weights must be 16-byte aligned");
   a.q = rows_of(q); a.k = rows_of(k); a.q_out = rows_of(q_out); a.k_out = rows_of(k_out);
   a.q_weight = q_weight; a.k_weight = k_weight; a.eps = eps;
   a.rows = rows; a.nlayers = nlayers; a.heads = params->num_heads; a.kv_heads = params->kv_heads;

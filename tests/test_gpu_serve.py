@@ -701,6 +701,54 @@ def test_calls_on_two_streams():
         assert serve.verify(*ask, workspace=shared)[1].tolist() == drawn[1].tolist()
 
 
+def test_captured_without_a_workspace():
+    # every call of a graph then has room of its own, cleared at each replay
+    lens, news = [5000, 3000], [2, 1]
+    table, pos, row0, pages = layout(lens, news, 4)
+    cache, params = random_cache(1, 1, pages, 8), paged.Params(1, 8, 1, io_dtype=BF16)
+    q = rows_of((1, row0[-1], 8, 64), 1, BF16)
+    args = (params, cache, q, i32(pos), i32(row0), i32(table), i32(lens), 2, 5000)
+    target, draft = probabilities(3, 20_000, 5, F32)
+    ask = (target, draft, i64([1, 2, 3]), i32(row0), torch.tensor([0.0, 0.5, 0.5], device=DEV), torch.tensor([0.3, 0.6], device=DEV))
+    want, drawn = serve.attend(*args), serve.verify(*ask)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        serve.attend(*args), serve.verify(*ask)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, got = serve.attend(*args), serve.verify(*ask)
+    for _ in range(3):
+        out.zero_()
+        got[1].zero_()
+        graph.replay()
+        assert torch.equal(out, want) and torch.equal(got[0], drawn[0]) and torch.equal(got[1], drawn[1])
+        assert torch.equal(serve.attend(*args), want)
+
+
+def test_broadcast_rows_and_strided_probabilities():
+    # queries, keys and values that several rows, heads or layers share; probabilities whose rows are further apart
+    cache, params = serve.Cache4(2, 3, 2), paged.Params(2, 6, 3, tq.rope_table(80), F16)
+    one = rows_of((1, 1, 1, 64), 3, F16)
+    k, q = one.expand(2, 70, 3, 64), one.expand(2, 70, 6, 64)
+    slots, pos = list(range(70)), list(range(70))
+    serve.append(params, cache, k, k, i64(slots), i32(pos))
+    whole = serve.Cache4(2, 3, 2)
+    serve.append(params, whole, k.contiguous(), k.contiguous(), i64(slots), i32(pos))
+    assert torch.equal(cache.k_codes, whole.k_codes) and torch.equal(cache.v_codes, whole.v_codes) and torch.equal(cache.scales, whole.scales)
+    rest = (i32(pos), i32([0, 70]), i32([[0, 1]]), i32([70]), 70, 70)
+    assert torch.equal(serve.attend(params, cache, q, *rest), serve.attend(params, cache, q.contiguous(), *rest))
+    for a, b in zip(serve.norm_rope(params, q, k, i32(pos)), serve.norm_rope(params, q.contiguous(), k.contiguous(), i32(pos))):
+        assert torch.equal(a, b)
+    with pytest.raises(tq.TQError, match="stride of zero"):
+        serve.norm_rope(params, q, k, i32(pos), out=(q, k))
+    target, draft = probabilities(12, 3001, 5, BF16)
+    ask = lambda p, d: serve.verify(p, d, i64([1, 2, 3, 4]), i32([0, 4]), torch.full((4,), 0.1, device=DEV), torch.full((1,), 0.7, device=DEV))
+    for a, b in zip(ask(target[::3], draft[::3]), ask(target[::3].contiguous(), draft[::3].contiguous())):
+        assert a is None or torch.equal(a, b)
+
+
 def test_a_cache_of_another_kind_is_refused():
     c8, c4 = paged.Cache(1, 1, 2), serve.Cache4(1, 1, 2)
     params = paged.Params(1, 1, 1)

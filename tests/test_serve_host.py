@@ -12,7 +12,7 @@ import torch
 import serve_ref as ref
 from paper_2603_26110_amd import TQError, paged, serve
 from test_code_hazards import OBJDUMP, _code_objects, too_early
-from test_paged_host import FAKE, P, _params, _ref, _rows
+from test_paged_host import FAKE, P, _params, _ref, _rows, stores_whose_data_is_written_next
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.skipif(not os.path.exists(serve.lib_path), reason="libturboesm_serve.so is not built")
@@ -49,6 +49,7 @@ def test_no_register_is_read_too_early(tmp_path):
         instructions += listing.count("\n\tv_")
         found = too_early(listing)
         assert not found, (len(found), found[:5])
+        assert not stores_whose_data_is_written_next(listing)
         assert "v_pk_fma_f32" not in listing and "v_pk_mul_f32" not in listing and "v_pk_add_f32" not in listing
     assert instructions > 5000
 
@@ -97,7 +98,8 @@ def verify(target=FAKE, ts=33, draft=FAKE, ds=33, io=0, vocab=33, rows=8, B=2, t
     (norm, dict(axes=1, sections=[31]), -2, "32"), (norm, dict(axes=2, sections=[2 ** 31 - 1, 2 ** 31 - 1]), -2, "32"),
     (norm, dict(q=None), -1, "q is NULL"), (norm, dict(k=_rows(data=None)), -1, "k is NULL"),
     (norm, dict(qo=None), -1, "q_out"), (norm, dict(ko=_rows(data=FAKE + 8)), -3, "k_out"),
-    (norm, dict(q=_rows(row=500)), -3, "multiples of 8"), (norm, dict(pos=0), -1, "pos"),
+    (norm, dict(qo=_rows(row=0)), -1, "q_out: a stride"), (norm, dict(ko=_rows(head=0)), -1, "k_out: a stride"),
+    (norm, dict(nlayers=2), -1, "q_out: a stride"), (norm, dict(q=_rows(row=500)), -3, "multiples of 8"), (norm, dict(pos=0), -1, "pos"),
     (norm, dict(qw=FAKE + 4), -3, "weights"), (norm, dict(kw=FAKE + 4), -3, "weights"),
     (norm, dict(rows=2 ** 31 - 1), -1, "too many"), (norm, dict(rows=2 ** 24, nlayers=3), -1, "too many"),
     (append, dict(p=None), -1, "params"), (append, dict(c=None), -1, "cache"), (append, dict(c=_cache(k_codes=0)), -1, "NULL"),
