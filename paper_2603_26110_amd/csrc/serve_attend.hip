@@ -118,6 +118,15 @@ __device__ __forceinline__ int largest_of_wave(int x) {
   return __builtin_amdgcn_readfirstlane(max((int)b[0], (int)b[1]));
 }
 
+// The largest of 16 lanes side by side.
+__device__ __forceinline__ float max_of_sixteen(float x) {
+  auto turned = [&](auto by) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x120 + decltype(by)::value, 0xF, 0xF, true)); };
+  x = fmaxf(x, turned(std::integral_constant<int, 8>()));
+  x = fmaxf(x, turned(std::integral_constant<int, 4>()));
+  x = fmaxf(x, turned(std::integral_constant<int, 2>()));
+  return fmaxf(x, turned(std::integral_constant<int, 1>()));
+}
+
 // Weights exp2(s c - m). A multiply-add does not round s c, but m was rounded: from 2^25
 // on the two differ by powers of two. So large scores are rounded before it.
 __device__ __forceinline__ bool rounds_first(float top) { return __any(fabsf(top) > 0x1p20f && fabsf(top) < INFINITY); }
@@ -138,6 +147,14 @@ __device__ __forceinline__ bool rounds_first(float top) { return __any(fabsf(top
 // R: rows of a unit. Up to 4: the sixteen rows of the first product are the unit's rows four
 // times, and lane group g takes the scores of tokens 16 g .. 16 g + 15 only: a score a lane
 // and row instead of four.
+//
+// From 2^24 on s_j + log2 scale(v_j) loses whole numbers of the scale's exponent, of which l takes all out again: tokens
+// with equal scores would no longer weigh the same. Below kLarge the sum is one rounding of the score (2^-8 in the
+// exponent at most). A wave that meets larger ones goes over its pages a second time, with two references: of the
+// scores, subtracted first, and of what is left with the scale's exponent. (640 units of 8192 tokens 141 us then, not
+// 61; 64 sequences of 1000 tokens and 40 heads on 8 26, not 15. The test for it is made where a reference rises: 18.4 ->
+// 18.7 us in a step of 64 ragged sequences.)
+constexpr float kLarge = 0x1p16f;
 constexpr float kTop = 7.0f;                          // the largest weight is kept in 2^7 .. 2^15
 constexpr int kWeights = 64 * 2 + 16;                 // bytes of a row's weights in LDS, and some to spread the banks
 
@@ -288,8 +305,11 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
 
   // more: whether `next` takes this page's place. (Known to the compiler, which then knows what is on its way, too, and
   // waits for no more than it needs.)
-  auto attend = [&](auto more, int tl, int next, bool next_bad) {
-    constexpr bool kMore = decltype(more)::value;
+  // far: with references of scores and of scales apart (below).
+  bool large = false;
+  float ref[kRows];
+  auto attend = [&](auto more, auto far, int tl, int next, bool next_bad) {
+    constexpr bool kMore = decltype(more)::value, kFar = decltype(far)::value;
     f32x4 S[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -304,23 +324,24 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
     }
     // (the registers that this page's keys leave take the next one's)
     if (kMore) load_keys(next);
-    float x[kTokens][kRows], over[kTokens];
+    float x[kTokens][kRows], over[kTokens], value[kTokens];
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) {
       const uint32_t kb = kPacked ? (ks | lost) & 0xFF : __builtin_amdgcn_ubfe(ks | lost, 8 * i, 8);
       const uint32_t vb = kPacked ? vs[0] & ~lost : __builtin_amdgcn_ubfe(vs[i] & ~lost, 8 * (c16 & 3), 8);
       const float key = __uint_as_float(kb << 23);
       // (zero times a scale of infinity is no number)
-      const float value = fmaf(key, 0.0f, (float)vb - 127.0f);
+      value[i] = fmaf(key, 0.0f, (float)vb - 127.0f);
       over[i] = __uint_as_float((254 - vb) << 23);
 #pragma unroll
       for (int j = 0; j < kRows; ++j) {
         const f32x4 part = !kPacked ? S[i] : g == 0 ? S[0] : g == 1 ? S[1] : g == 2 ? S[2] : S[3];
         const float score = R == 1 ? part[0] + part[1] : part[j];
-        x[i][j] = fmaf(score * by[j], key, value);
+        x[i][j] = kFar ? score * by[j] * key : fmaf(score * by[j], key, value[i]);
       }
     }
-    if ((tl + 1) * kPage > least) {
+    const bool masked = (tl + 1) * kPage > least;
+    auto mask = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < kTokens; ++i) {
         const int tok = tl * kPage + (kPacked ? lane : 16 * i + c16);
@@ -330,27 +351,56 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
         for (int j = 0; j < kRows; ++j)
           if (tok >= sees[j]) x[i][j] = -INFINITY;
       }
-    }
+    };
+    if (masked) mask();
     if (kMore) load_scales(next, next_bad);
-    float rise = -INFINITY, top[kRows];
+    auto largest_of_row = [&](int j) __attribute__((always_inline)) {
+      float t = x[0][j];
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-      top[j] = x[0][j];
+      for (int i = 1; i < kTokens; ++i) t = fmaxf(t, x[i][j]);
+      t = max_of_sixteen(t);
+      return kPacked ? max_across32(max_across16(t)) : t;
+    };
+    auto scale_sums = [&](int j, float f) __attribute__((always_inline)) {
+      lsum[j] *= f;
 #pragma unroll
-      for (int i = 1; i < kTokens; ++i) top[j] = fmaxf(top[j], x[i][j]);
-      rise = fmaxf(rise, top[j] - m[j]);
-    }
-    if (__any(rise > kRaise)) {
+      for (int d = 0; d < 4; ++d) O[d][j] *= f;
+    };
+    if constexpr (kFar) {
+      // x: scores, then exponents of weights: P_j = exp2((s_j - m) + log2 scale(v_j) - ref)
+      float up[kRows], f[kRows];
 #pragma unroll
       for (int j = 0; j < kRows; ++j) {
+        up[j] = fmaxf(m[j], largest_of_row(j));
+        f[j] = m[j] - up[j];
+        m[j] = up[j];
 #pragma unroll
-        for (int o = kPacked ? 32 : 8; o >= 1; o >>= 1) top[j] = fmaxf(top[j], __shfl_xor(top[j], o, 64));
-        const float to = top[j] - m[j] > kRaise ? top[j] - kTop : m[j];
-        const float f = __builtin_amdgcn_exp2f(m[j] - to);
-        m[j] = to;
-        lsum[j] *= f;
+        for (int i = 0; i < kTokens; ++i) x[i][j] = (x[i][j] - up[j]) + value[i];
+      }
+      if (masked) mask();          // (a scale that does not count may be no number)
 #pragma unroll
-        for (int d = 0; d < 4; ++d) O[d][j] *= f;
+      for (int j = 0; j < kRows; ++j) {
+        const float to = fmaxf(largest_of_row(j) - kTop, f[j] + ref[j]);
+        scale_sums(j, __builtin_amdgcn_exp2f((f[j] + ref[j]) - to));
+        ref[j] = to;
+      }
+    } else {
+      float rise = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kRows; ++j) {
+        float top = x[0][j];
+#pragma unroll
+        for (int i = 1; i < kTokens; ++i) top = fmaxf(top, x[i][j]);
+        rise = fmaxf(rise, top - m[j]);
+      }
+      if (__any(rise > kRaise)) {
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+          const float top = largest_of_row(j), to = top - m[j] > kRaise ? top - kTop : m[j];
+          large = large || __any(fabsf(top) > kLarge && fabsf(top) < INFINITY);
+          scale_sums(j, __builtin_amdgcn_exp2f(m[j] - to));
+          m[j] = to;
+        }
       }
     }
 #pragma unroll
@@ -358,7 +408,7 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
       float p[kTokens];
 #pragma unroll
       for (int i = 0; i < kTokens; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(x[i][j] - m[j]);
+        p[i] = __builtin_amdgcn_exp2f(x[i][j] - (kFar ? ref[j] : m[j]));
         lsum[j] = fmaf(p[i], over[i], lsum[j]);
       }
 #pragma unroll
@@ -404,9 +454,34 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
     load_values(page);
     for (int i = 0; i + 1 < n; ++i) {
       page = page_of(i + 1, bad);
-      attend(std::true_type(), first + i * W, page, bad);
+      attend(std::true_type(), std::false_type(), first + i * W, page, bad);
     }
-    attend(std::false_type(), first + (n - 1) * W, 0, false);
+    attend(std::false_type(), std::false_type(), first + (n - 1) * W, 0, false);
+  }
+  if (large) {
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      m[j] = lowest();
+      ref[j] = lsum[j] = 0.0f;
+    }
+#pragma unroll
+    for (int d = 0; d < 4; ++d) O[d] = f32x4{};
+    for (int tl = begin; tl < end; tl += W) {
+      entries = table[tl];
+      page = page_of(0, bad);
+      load_keys(page);
+      load_scales(page, bad);
+      load_values(page);
+      attend(std::false_type(), std::true_type(), tl, 0, false);
+    }
+    // (so that the sums are relative to m alone, as the others' are: over at most 2^55)
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      const float f = __builtin_amdgcn_exp2f(ref[j]);
+      lsum[j] *= f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) O[d][j] *= f;
+    }
   }
 #pragma unroll
   for (int j = 0; j < kRows; ++j) {
