@@ -65,7 +65,8 @@ TQ_API int64_t tqs_cache_bytes(int32_t num_layers, int32_t kv_heads, int64_t pag
  *   y = x * weight / sqrt(mean(x^2) + eps)     (mean over the 64 dimensions)
  *   pair m of y is turned by the angle of params->rope_cs[pos[axis(m)][row]][m]
  * in binary32, rounded once to io_dtype. (The squares are, too: entries past 2^60
- * may overflow them, and with eps 0 a head of zeros is NaN.) Pairs are (2m, 2m+1), or (m, m+32)
+ * may overflow them. With eps 0 a head of zeros is NaN, and one whose entries are all
+ * below 2^-60 may lose digits of its squares, or all of them: then it is infinite.) Pairs are (2m, 2m+1), or (m, m+32)
  * with TQ_ROPE_HALF. The first sections[0] pairs take axis 0, the next
  * sections[1] axis 1, and so on (time, height and width, say). Without rope_cs
  * nothing is turned. What comes out goes to tqs_append, tqs_attend and their

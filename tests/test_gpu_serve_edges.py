@@ -9,7 +9,7 @@ import paged_ref
 import serve_ref as ref
 import paper_2603_26110_amd as tq
 from paper_2603_26110_amd import paged, serve
-from test_gpu_serve import BF16, DEV, F16, F32, i32, i64, layout, random_cache, rows_of
+from test_gpu_serve import BF16, DEV, F16, F32, angles, check_norm, i32, i64, layout, random_cache, rows_of
 
 pytestmark = pytest.mark.gpu
 
@@ -140,3 +140,22 @@ def test_one_key_decides(name, io, fp32_out):
             assert bool((off <= most)[sure].all()), (b, r, float((off / most)[sure].max()))
             asked, told = asked + sure.numel(), told + int(sure.sum())
     assert told >= asked / 2, (told, asked)
+
+
+# ------------------------------------------------------------------ norm_rope
+@pytest.mark.parametrize("rope", ["none", "pairs", "half"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_over_the_range_of_its_squares(dtype, rope):
+    # eps 0, heads whose largest entry is from 2^-60 to 2^60: their squares are binary32's (the lowest steps, 2^-149, are
+    # 64 * 2^-150 of a sum of 2^-120, within its rounding), in rows of one call
+    powers = [-60, -59, -40, 0, 40, 59, 60]
+    x = rows_of((1, len(powers), 3, 64), 4, F32)
+    x = (x / x.abs().amax(-1, keepdim=True)).double()
+    x[..., 5] = 1.0
+    x = (x * 2.0 ** torch.tensor(powers, dtype=torch.float64, device=DEV)[:, None, None]).to(dtype)
+    cs = None if rope == "none" else tq.rope_table(9)
+    params = paged.Params(1, 3, 3, cs, dtype, tq.ROPE_HALF if rope == "half" else 0)
+    pos = i32([3] * len(powers))
+    z = None if cs is None else angles(9)[pos.long()]
+    for got in serve.norm_rope(params, x, x, pos, eps=0.0):
+        check_norm(got, x, None, 0.0, z, rope == "half")
