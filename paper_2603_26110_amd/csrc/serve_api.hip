@@ -149,6 +149,7 @@ tq_status tqs_norm_rope(const tqp_params* params, const tqp_rows* q, const tqp_r
   }
   if (rows == 0 || nlayers == 0) return ok();
   if ((s = check_rows(q, "q")) != TQ_OK || (s = check_rows(k, "k")) != TQ_OK) return s;
+  // (the documented limit: below the 2^32 threads of a launch, which has a wave for every sixteen heads)
   const int64_t eights = ((int64_t)params->num_heads + params->kv_heads + 7) / 8;
   if (rows > (((int64_t)1 << 26) - 1) / nlayers / eights) return fail(TQ_ERR_ARG, "too many rows for one call");
   if ((s = check_out(q_out, "q_out", nlayers, rows, params->num_heads)) != TQ_OK) return s;

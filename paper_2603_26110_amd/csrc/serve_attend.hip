@@ -17,7 +17,10 @@
 // of as much takes 57 (the 8-bit cache 119); 660 of 1025 tokens 14 us (19); 20 of 1025 tokens
 // 8.3 us, a chain of latencies; 512 ragged ones of up to 2001 tokens and five rows 19 us. Four
 // chunks of up to 512 rows on up to 4000 tokens (33 GFLOP), bf16 83 us; every token of 1024
-// with every other in 33 layers of 20 heads (177 GFLOP), bf16 339 us, fp16 490.
+// with every other in 33 layers of 20 heads (177 GFLOP), bf16 329 us, fp16 476, fp32 568 (the
+// 8-bit cache's attention: bf16 245, fp16 313). Bound by vector work there: by counters 282
+// vector instructions a wave and page in bf16, about 1500 cycles with 32 exponentials at a quarter of
+// the rate, of 1900, beside 512 of the matrix cores; 392 (1950 of 2740, 1024) in fp16.
 //
 // The cache is in the Hadamard basis. A query row is brought there once (64 entries,
 // six butterflies, mostly within a lane), its result back once.
@@ -532,7 +535,9 @@ __global__ __launch_bounds__(W * 64, R > 4 ? 3 : 4) void attend4_few(Attend4Args
 //
 // Here scales go into the operands, once a page for all rows. Values are bf16, which has
 // binary32's exponents, so that a token's scale need not be brought in line with
-// another's; the weights are in one or more bf16 parts. Keys are fp16, so that a query in one part (2^-12
+// another's; the weights are in one or more bf16 parts: one for bf16 results, whose own rounding is as large
+// (the row's sum takes the weights as rounded, so that they add up to one), two for fp16 and three for fp32. Keys
+// are fp16, so that a query in one part (2^-11
 // of an entry) is enough for bf16 results, over a power of two a page that puts its largest
 // scale at 2^13: exact for scales down to 2^-36 of it. A page with smaller ones has its codes
 // staged as they are and its scores multiplied afterwards (as whole numbers of the

@@ -1,4 +1,4 @@
-// Device helpers of the 4-bit cache: its layout, its codes, and vectors that eight
+// Device helpers of the 4-bit cache: its layout, its codes, and vectors that four
 // lanes hold together.
 #pragma once
 
